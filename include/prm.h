@@ -60,7 +60,8 @@ extern "C" {
 #define PRM_ENOMEM (-4)  /* workspace does not fit the budget or the device */
 #define PRM_EHIP   (-5)  /* a HIP runtime call failed; the message carries its error string */
 
-typedef enum prm_dtype { PRM_F32 = 0, PRM_BF16 = 1 } prm_dtype;
+/* PRM_F16: activations and outputs of the 8-bit linear layer's operators only. */
+typedef enum prm_dtype { PRM_F32 = 0, PRM_BF16 = 1, PRM_F16 = 2 } prm_dtype;
 
 /* Shape scale s(W) of eq. (periodic-direction); the paper names it a
  * scale that depends on the matrix shape, without a formula. */
@@ -312,6 +313,80 @@ int prm_peak_hbm(void* hip_stream, uint64_t bytes, double* read_gbs, double* wri
 #define PRM_NOALLOC_SCRATCH_BYTES (256ull << 20)
 int prm_step_noalloc(const prm_config* cfg, int64_t rows, int64_t cols, void* param, const void* grad,
                      float* momentum, int64_t step, float lr, int32_t* did_refresh, void* hip_stream);
+
+/* ---- 8-bit linear layer ---------------------------------------------------
+ * The operators that a linear layer computed in 8 bits takes beside the step
+ * that trains its weight: a quantiser, the product of 8-bit operands, and the
+ * root-mean-square norm in front of it.  No context: each call enqueues its
+ * kernels on `hip_stream`, on the CURRENT device, allocates nothing and never
+ * waits for the GPU, so it may be captured into a HIP graph.  Calls share no
+ * memory but what the caller hands them, and may run at once on several
+ * threads and streams as long as their outputs and workspaces are not the same.
+ *
+ * Matrices are row-major with a leading dimension in ELEMENTS (>= the row's
+ * length); a row may start at any address its element type allows, and what
+ * lies between rows and behind the last one is neither read nor written.
+ * Outputs must not overlap inputs or each other.  `dtype` is the prm_dtype of
+ * activations, norm weights, biases and outputs (fp32, bf16, fp16); scales are
+ * fp32.  Sizes: 0 <= rows <= 2^31 - 1 (0: nothing is done), 1 <= cols <= 2^24,
+ * unless stated.  Device pointers are checked with hipPointerGetAttributes; a
+ * failed call has enqueued nothing.  Errors as in prm_step (PRM_EINVAL,
+ * PRM_EDTYPE; PRM_EALIGN: not on an element's boundary; PRM_EHIP).
+ *
+ * 8 bits: a row v is held as whole numbers q in [-127, 127] and one scale,
+ *   s = max|v| / 127,   q = rn(127 v / max|v|)   (to nearest, ties to even),
+ * decided exactly also where a value lies next to the border of two whole
+ * numbers.  A row of zeros has s = 0 and q = 0; a row with an infinity or a
+ * NaN has s = NaN and q = 0, so that it stays visible in every product. */
+
+/* x (rows x cols) in 8 bits, a scale for each row: q (rows x cols, leading
+ * dimension ldq), scale (rows). */
+int prm_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx,
+                      int8_t* q, int64_t ldq, float* scale, void* hip_stream);
+
+/* x in 8 bits with a scale for each COLUMN, transposed: q (cols x rows, leading
+ * dimension ldq >= rows), scale (cols), and, unless `sum` is NULL, the columns'
+ * sums over the rows (cols values of type dtype, added in fp32 in a fixed order; the
+ * gradient of a bias).  1 <= rows <= 2^22, cols <= 2^24.  `workspace`:
+ * prm_quantize_cols_workspace(rows, cols) bytes, 16-byte aligned, used by this
+ * call only. */
+uint64_t prm_quantize_cols_workspace(int64_t rows, int64_t cols);
+int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx,
+                      int8_t* q, int64_t ldq, float* scale, void* sum, void* workspace,
+                      uint64_t workspace_bytes, void* hip_stream);
+
+/* out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] b[j][k] + bias[j], for a
+ * (m x k: tokens), b (n x k: output channels, as a linear layer's weight is kept)
+ * and out (m x n, type dtype).  The sum is exact (32-bit whole numbers: 1 <= k <=
+ * 131071, where 128 * 128 k still fits), the rest fp32, rounded once.  bias: n values
+ * of type dtype, or NULL.  0 <= m, n <= 2^24. */
+int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
+                    const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo,
+                    int64_t m, int64_t n, int64_t k, void* hip_stream);
+
+/* Root-mean-square norm of each row of x (rows x cols), after the residual's
+ * addition where `residual` is not NULL:
+ *   h = x + residual          (rounded to dtype and written to h; else h = x)
+ *   y = h * w / sqrt(mean(h^2) + eps)    (w: cols values, NULL: ones)
+ * written either to y (type dtype; q and scale NULL) or to q and scale in 8 bits
+ * (y NULL), as the quantiser would lay out the unrounded y.  The norm is that of the
+ * rounded h.  eps > 0.  The sum of squares is taken in fp32. */
+int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w,
+                 int32_t dtype, int64_t rows, int64_t cols, float eps, void* h, int64_t ldh,
+                 void* y, int64_t ldy, int8_t* q, int64_t ldq, float* scale, void* hip_stream);
+
+/* Gradients of prm_rms_norm's y (and kept sum): with r = 1 / sqrt(mean(h^2) + eps),
+ * n = h r and g = gy w,
+ *   dx = r (g - n mean(g n)) + gh      (gh: the gradient of the kept sum, or NULL;
+ *                                       dx is the residual's gradient too)
+ *   dw = sum over rows of gy n         (or dw NULL)
+ * both of type dtype; dw is added in fp32 in a fixed order.  `workspace`:
+ * prm_rms_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, used by this
+ * call only (may be NULL without dw).  rows = 0 writes dw = 0. */
+uint64_t prm_rms_norm_backward_workspace(int64_t rows, int64_t cols);
+int prm_rms_norm_backward(const void* gy, int64_t ldgy, const void* gh, int64_t ldgh, const void* h, int64_t ldh,
+                          const void* w, int32_t dtype, int64_t rows, int64_t cols, float eps, void* dx,
+                          int64_t lddx, void* dw, void* workspace, uint64_t workspace_bytes, void* hip_stream);
 
 /* Message of the last failing call on this thread ("" if none). */
 const char* prm_last_error(void);

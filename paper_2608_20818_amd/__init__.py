@@ -16,13 +16,15 @@ __all__ = [
     "PRMError", "Config", "KernelStats", "Optimizer", "AdamWConfig", "AuxAdamW", "load",
     "config_default", "adamw_config_default",
     "schedule_is_refresh", "plan_workspace_bytes", "step_noalloc", "NOALLOC_SCRATCH_BYTES", "PRM_OK", "PRM_EINVAL", "PRM_EDTYPE", "PRM_EALIGN",
-    "PRM_ENOMEM", "PRM_EHIP", "F32", "BF16", "KERNEL_CLASSES",
+    "PRM_ENOMEM", "PRM_EHIP", "F32", "BF16", "F16", "KERNEL_CLASSES",
+    "quantize_rows", "int8_matmul", "int8_linear", "rms_norm",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libprm.so")
 
 PRM_OK, PRM_EINVAL, PRM_EDTYPE, PRM_EALIGN, PRM_ENOMEM, PRM_EHIP = 0, -1, -2, -3, -4, -5
 F32, BF16 = 0, 1
+F16 = 2  # the 8-bit linear layer's operators only
 SCALE_ONE, SCALE_SQRT_ASPECT, SCALE_RMS_0P2 = 0, 1, 2
 NUM_KERNEL_CLASSES = 11
 NOALLOC_SCRATCH_BYTES = 256 << 20  # PRM_NOALLOC_SCRATCH_BYTES
@@ -120,6 +122,18 @@ def load() -> ctypes.CDLL:
     L.prm_adamw_step.restype = ctypes.c_int
     L.prm_adamw_destroy.argtypes = [P]
     L.prm_adamw_destroy.restype = ctypes.c_int
+    i64, i32, u64, f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float
+    L.prm_quantize_rows.argtypes = [P, i32, i64, i64, i64, P, i64, P, P]
+    L.prm_quantize_cols_workspace.argtypes = [i64, i64]
+    L.prm_quantize_cols_workspace.restype = u64
+    L.prm_quantize_cols.argtypes = [P, i32, i64, i64, i64, P, i64, P, P, P, u64, P]
+    L.prm_int8_matmul.argtypes = [P, i64, P, P, i64, P, P, i32, P, i64, i64, i64, i64, P]
+    L.prm_rms_norm.argtypes = [P, i64, P, i64, P, i32, i64, i64, f32, P, i64, P, i64, P, i64, P, P]
+    L.prm_rms_norm_backward_workspace.argtypes = [i64, i64]
+    L.prm_rms_norm_backward_workspace.restype = u64
+    L.prm_rms_norm_backward.argtypes = [P, i64, P, i64, P, i64, P, i32, i64, i64, f32, P, i64, P, P, u64, P]
+    for name in ("prm_quantize_rows", "prm_quantize_cols", "prm_int8_matmul", "prm_rms_norm", "prm_rms_norm_backward"):
+        getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
 
@@ -411,7 +425,11 @@ class AuxAdamW:
 
 
 def __getattr__(name):
-    # the torch.optim adapter imports torch; load it on first use
+    # the torch.optim adapter and the operators import torch; load them on first use
+    if name in ("quantize_rows", "int8_matmul", "int8_linear", "rms_norm"):
+        from . import operators
+        fn = globals()[name] = getattr(operators, name)
+        return fn
     if name == "PRMOptimizer":
         from .torch_optim import PRMOptimizer
         return PRMOptimizer

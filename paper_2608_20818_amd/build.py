@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libprm.so")
-SOURCES = ("prm_api.hip", "rowwise.hip", "ns5.hip", "ns5_small.hip", "probe.hip", "adamw.hip")
+SOURCES = ("prm_api.hip", "rowwise.hip", "ns5.hip", "ns5_small.hip", "probe.hip", "adamw.hip",
+           "ops_api.hip", "ops_rows.hip", "ops_matmul.hip")
 ARCH = "gfx950"
 
 FLAGS = [

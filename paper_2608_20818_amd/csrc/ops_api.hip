@@ -1,0 +1,210 @@
+// C ABI of the 8-bit linear layer's operators (declared in include/prm.h):
+// argument checks, workspace layout and launches.  No state of their own.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "../../include/prm.h"
+#include "ops_internal.h"
+
+using namespace prm;
+
+namespace {
+
+constexpr int64_t kMaxCols = 1ll << 24, kMaxRows = (1ll << 31) - 1, kMaxColRows = 1ll << 22;
+
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+int fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return set_error(code, buf);
+}
+
+int check_type(int32_t t) {
+  return t == PRM_F32 || t == PRM_BF16 || t == PRM_F16 ? PRM_OK : fail(PRM_EDTYPE, "unsupported dtype %d", t);
+}
+int64_t size_of(int32_t t) { return t == PRM_F32 ? 4 : 2; }
+
+struct Buf {
+  const void* p;
+  const char* name;
+  int64_t align;
+};
+
+// Every buffer is memory of the current device, on its element's boundary.
+template <int N>
+int check_buffers(const char* call, const Buf (&b)[N]) {
+  for (int i = 0; i < N; ++i) {
+    if (!b[i].name) continue;  // an optional one that is not there
+    if (!b[i].p) return fail(PRM_EINVAL, "%s: %s is NULL", call, b[i].name);
+    if ((uintptr_t)b[i].p % b[i].align)
+      return fail(PRM_EALIGN, "%s: %s is not %lld-byte aligned", call, b[i].name, (long long)b[i].align);
+  }
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail(PRM_EHIP, "hipGetDevice failed: %s", hipGetErrorString(e));
+  for (int i = 0; i < N; ++i)
+    if (b[i].name)
+      if (const int rc = device_pointer(dev, b[i].p, call, 0, i)) return rc;
+  return PRM_OK;
+}
+Buf optional(const void* p, const char* name, int64_t align) { return Buf{p, p ? name : nullptr, align}; }
+
+int check_rows(const char* call, int64_t rows, int64_t cols, int64_t least_rows = 0, int64_t most_rows = kMaxRows) {
+  if (rows < least_rows || rows > most_rows || cols < 1 || cols > kMaxCols)
+    return fail(PRM_EINVAL, "%s: invalid shape %lld x %lld", call, (long long)rows, (long long)cols);
+  return PRM_OK;
+}
+int check_ld(const char* call, const char* name, int64_t ld, int64_t least) {
+  return ld >= least ? PRM_OK
+                     : fail(PRM_EINVAL, "%s: leading dimension %s = %lld, needs %lld or more", call, name, (long long)ld, (long long)least);
+}
+int launched(const char* call, hipError_t e) {
+  return e == hipSuccess ? PRM_OK : fail(PRM_EHIP, "%s: launch failed: %s", call, hipGetErrorString(e));
+}
+int check_workspace(const char* call, const void* p, uint64_t have, uint64_t need) {
+  if (have < need || !p)
+    return fail(PRM_EINVAL, "%s: the workspace has %llu bytes, needs %llu", call, (unsigned long long)(p ? have : 0),
+                (unsigned long long)need);
+  return PRM_OK;
+}
+
+#define TRY(expr)                    \
+  do {                               \
+    const int rc_ = (expr);          \
+    if (rc_ != PRM_OK) return rc_;   \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int prm_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* q, int64_t ldq,
+                      float* scale, void* hip_stream) {
+  static const char* const call = "prm_quantize_rows";
+  TRY(check_type(dtype));
+  TRY(check_rows(call, rows, cols));
+  TRY(check_ld(call, "ldx", ldx, cols));
+  TRY(check_ld(call, "ldq", ldq, cols));
+  if (rows == 0) return PRM_OK;
+  TRY(check_buffers(call, {{x, "x", size_of(dtype)}, {q, "q", 1}, {scale, "scale", 4}}));
+  QuantArgs a = {};
+  a.x = x;
+  a.q = q;
+  a.scale = scale;
+  a.rows = rows;
+  a.cols = cols;
+  a.ldx = ldx;
+  a.ldq = ldq;
+  return launched(call, launch_quantize_rows((OpType)dtype, a, (hipStream_t)hip_stream));
+}
+
+uint64_t prm_quantize_cols_workspace(int64_t rows, int64_t cols) {
+  if (rows < 1 || rows > kMaxColRows || cols < 1 || cols > kMaxCols) return 0;
+  int32_t nrb, per;
+  quantize_cols_blocks(rows, cols, &nrb, &per);
+  return (uint64_t)nrb * (uint64_t)cols * 8;
+}
+
+int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* q, int64_t ldq,
+                      float* scale, void* sum, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  static const char* const call = "prm_quantize_cols";
+  TRY(check_type(dtype));
+  TRY(check_rows(call, rows, cols, 1, kMaxColRows));
+  TRY(check_ld(call, "ldx", ldx, cols));
+  TRY(check_ld(call, "ldq", ldq, rows));
+  TRY(check_workspace(call, workspace, workspace_bytes, prm_quantize_cols_workspace(rows, cols)));
+  TRY(check_buffers(call, {{x, "x", size_of(dtype)}, {q, "q", 1}, {scale, "scale", 4}, optional(sum, "sum", size_of(dtype)),
+                           {workspace, "workspace", 16}}));
+  QuantArgs a = {};
+  a.x = x;
+  a.q = q;
+  a.scale = scale;
+  a.sum = sum;
+  a.rows = rows;
+  a.cols = cols;
+  a.ldx = ldx;
+  a.ldq = ldq;
+  quantize_cols_blocks(rows, cols, &a.nrb, &a.rows_per_block);
+  a.part_max = (uint32_t*)workspace;
+  a.part_sum = (float*)workspace + (int64_t)a.nrb * cols;
+  return launched(call, launch_quantize_cols((OpType)dtype, a, (hipStream_t)hip_stream));
+}
+
+int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
+                    const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m, int64_t n, int64_t k,
+                    void* hip_stream) {
+  static const char* const call = "prm_int8_matmul";
+  TRY(check_type(dtype));
+  if (m < 0 || n < 0 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK)
+    return fail(PRM_EINVAL, "%s: invalid sizes m %lld, n %lld, k %lld (1 <= k <= %lld)", call, (long long)m, (long long)n,
+                (long long)k, (long long)kMaxProductK);
+  TRY(check_ld(call, "lda", lda, k));
+  TRY(check_ld(call, "ldb", ldb, k));
+  TRY(check_ld(call, "ldo", ldo, n));
+  if (m == 0 || n == 0) return PRM_OK;
+  TRY(check_buffers(call, {{a, "a", 1}, {a_scale, "a_scale", 4}, {b, "b", 1}, {b_scale, "b_scale", 4},
+                           optional(bias, "bias", size_of(dtype)), {out, "out", size_of(dtype)}}));
+  ProductArgs p = {a, b, a_scale, b_scale, bias, out, m, n, k, lda, ldb, ldo};
+  return launched(call, launch_int8_matmul((OpType)dtype, p, (hipStream_t)hip_stream));
+}
+
+int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w, int32_t dtype,
+                 int64_t rows, int64_t cols, float eps, void* h, int64_t ldh, void* y, int64_t ldy, int8_t* q, int64_t ldq,
+                 float* scale, void* hip_stream) {
+  static const char* const call = "prm_rms_norm";
+  TRY(check_type(dtype));
+  TRY(check_rows(call, rows, cols));
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PRM_EINVAL, "%s: eps must be finite and > 0", call);
+  if (!residual != !h) return fail(PRM_EINVAL, "%s: residual and h come together", call);
+  if (y ? (q || scale) : rows > 0 && !(q && scale)) return fail(PRM_EINVAL, "%s: either y, or q and scale", call);
+  TRY(check_ld(call, "ldx", ldx, cols));
+  if (residual) {
+    TRY(check_ld(call, "ldres", ldres, cols));
+    TRY(check_ld(call, "ldh", ldh, cols));
+  }
+  TRY(y ? check_ld(call, "ldy", ldy, cols) : check_ld(call, "ldq", ldq, cols));
+  if (rows == 0) return PRM_OK;
+  const int64_t es = size_of(dtype);
+  TRY(check_buffers(call, {{x, "x", es}, optional(residual, "residual", es), optional(w, "w", es), optional(h, "h", es),
+                           optional(y, "y", es), optional(q, "q", 1), optional(scale, "scale", 4)}));
+  NormArgs a = {x, residual, w, h, y, q, scale, rows, cols, ldx, ldres, ldh, ldy, ldq, eps};
+  return launched(call, launch_rms_norm((OpType)dtype, a, (hipStream_t)hip_stream));
+}
+
+uint64_t prm_rms_norm_backward_workspace(int64_t rows, int64_t cols) {
+  if (rows < 1 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return 0;
+  return (uint64_t)rms_norm_grad_parts(rows, cols) * (uint64_t)cols * 4;
+}
+
+int prm_rms_norm_backward(const void* gy, int64_t ldgy, const void* gh, int64_t ldgh, const void* h, int64_t ldh,
+                          const void* w, int32_t dtype, int64_t rows, int64_t cols, float eps, void* dx, int64_t lddx,
+                          void* dw, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  static const char* const call = "prm_rms_norm_backward";
+  TRY(check_type(dtype));
+  TRY(check_rows(call, rows, cols));
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PRM_EINVAL, "%s: eps must be finite and > 0", call);
+  TRY(check_ld(call, "ldgy", ldgy, cols));
+  TRY(check_ld(call, "ldh", ldh, cols));
+  TRY(check_ld(call, "lddx", lddx, cols));
+  if (gh) TRY(check_ld(call, "ldgh", ldgh, cols));
+  if (rows == 0 && !dw) return PRM_OK;
+  const int64_t es = size_of(dtype);
+  if (rows == 0) {
+    TRY(check_buffers(call, {{dw, "dw", es}}));
+  } else {
+    if (dw) TRY(check_workspace(call, workspace, workspace_bytes, prm_rms_norm_backward_workspace(rows, cols)));
+    TRY(check_buffers(call, {{gy, "gy", es}, optional(gh, "gh", es), {h, "h", es}, optional(w, "w", es), {dx, "dx", es},
+                             optional(dw, "dw", es), optional(dw ? workspace : nullptr, "workspace", 16)}));
+  }
+  NormGradArgs a = {gy, gh, h, w, dx, dw, (float*)workspace, rows, cols, ldgy, ldgh, ldh, lddx, eps,
+                    rms_norm_grad_parts(rows, cols)};
+  return launched(call, launch_rms_norm_grad((OpType)dtype, a, (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,76 @@
+// Internal definitions of the operators beside the optimizer step (ops_*.hip): the
+// 8-bit linear layer's quantiser, norm and product.  Their C ABI is in prm.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace prm {
+
+// prm_dtype of an operator's activations and outputs
+enum OpType : int32_t { OP_F32 = 0, OP_BF16 = 1, OP_F16 = 2 };
+
+// ---- error state shared with the optimizer step (prm_api.hip) ----------------
+int set_error(int code, const char* msg);  // stores msg for prm_last_error, returns code
+int device_pointer(int dev, const void* p, const char* what, int i, int k);  // PRM_OK or PRM_EINVAL
+
+// ---- rows (ops_rows.hip) ------------------------------------------------------
+// A row of `cols` elements; leading dimensions in elements, any alignment of an element.
+struct NormArgs {
+  const void* x;
+  const void* res;  // or nullptr
+  const void* w;    // or nullptr: ones
+  void* h;          // x + res in the storage type; with res only
+  void* y;          // or nullptr: q and scale instead
+  int8_t* q;
+  float* scale;
+  int64_t rows, cols, ldx, ldres, ldh, ldy, ldq;
+  float eps;
+};
+hipError_t launch_rms_norm(OpType t, const NormArgs& a, hipStream_t s);
+
+struct QuantArgs {
+  const void* x;
+  int8_t* q;
+  float* scale;
+  int64_t rows, cols, ldx, ldq;
+  // of the columns' form: partial maxima (and sums) of row blocks, nrb x cols each
+  uint32_t* part_max;
+  float* part_sum;
+  void* sum;  // column sums in the type of x, or nullptr
+  int32_t nrb, rows_per_block;
+};
+hipError_t launch_quantize_rows(OpType t, const QuantArgs& a, hipStream_t s);
+hipError_t launch_quantize_cols(OpType t, const QuantArgs& a, hipStream_t s);
+// row blocks of the columns' statistics
+void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block);
+
+struct NormGradArgs {
+  const void* gy;
+  const void* gh;  // gradient of the kept sum, or nullptr
+  const void* h;
+  const void* w;   // or nullptr
+  void* dx;
+  void* dw;        // or nullptr
+  float* part;     // nparts x cols
+  int64_t rows, cols, ldgy, ldgh, ldh, lddx;
+  float eps;
+  int32_t nparts;
+};
+hipError_t launch_rms_norm_grad(OpType t, const NormGradArgs& a, hipStream_t s);
+int32_t rms_norm_grad_parts(int64_t rows, int64_t cols);
+
+// ---- products (ops_matmul.hip) -------------------------------------------------
+struct ProductArgs {
+  const int8_t* a;  // m x k
+  const int8_t* b;  // n x k
+  const float* a_scale;
+  const float* b_scale;
+  const void* bias;  // n of the output's type, or nullptr
+  void* out;         // m x n
+  int64_t m, n, k, lda, ldb, ldo;
+};
+hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, hipStream_t s);
+constexpr int64_t kMaxProductK = 131071;  // 128 * 128 * k stays below 2^31
+
+}  // namespace prm

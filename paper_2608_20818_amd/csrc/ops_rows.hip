@@ -1,0 +1,591 @@
+// Row operators of the 8-bit linear layer on gfx950: the quantiser, and the
+// root-mean-square norm with the residual's addition and its gradients.
+//
+//   quantize    s = max |x| / 127 of the row,  q = rn(127 x / max |x|)
+//   rms_norm    h = x + res (kept in the storage type),  r = (mean h^2 + eps)^(-1/2)
+//               y = h r w, or y in 8 bits: as r is one number for the row, it cancels
+//               from q = rn(127 h w / max |h w|) and stays in the scale r max |h w| / 127
+//   gradient    n = h r, g = gy w:  dx = r (g - n mean(g n)) + gh,  dw = sum over rows of gy n
+//
+// All are bound by HBM: each element is read once and held in registers as stored
+// until the row's statistics are there (rows of at most 32768 elements; longer ones
+// are swept again).  A thread holds pieces of 8 elements, so that an access of 16-bit
+// values is 16 bytes a lane and one contiguous span a wave, at any alignment.
+#include <type_traits>
+
+#include "ops_device.h"
+
+namespace prm {
+namespace {
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off, 64));
+  return v;
+}
+__device__ __forceinline__ double wave_max(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
+  return v;
+}
+
+// The largest |u|, that keeps a NaN: fp32 magnitudes as their bits (NaN above infinity
+// above the finite ones), fp64 ones with a flag in the place of NaN (infinity).
+template <typename U> struct Top;
+template <> struct Top<float> {
+  uint32_t m = 0;
+  __device__ __forceinline__ void add(float u) { m = max(m, __float_as_uint(u) & 0x7fffffffu); }
+  __device__ __forceinline__ float value() const { return __uint_as_float(m); }
+};
+template <> struct Top<double> {
+  double m = 0;
+  __device__ __forceinline__ void add(double u) { m = u == u ? fmax(m, fabs(u)) : (double)__builtin_huge_valf(); }
+  __device__ __forceinline__ double value() const { return m; }
+};
+
+// Sum, and largest, over the threads of a row: a wave, or the whole block.
+template <int TPR, typename U>
+__device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_top, float* rs, decltype(Top<U>::m)* rt) {
+  ss = wave_sum(ss);
+  if (with_top) top.m = wave_max(top.m);
+  if constexpr (TPR > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      rs[w] = ss;
+      if (with_top) rt[w] = top.m;
+    }
+    __syncthreads();
+    ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < TPR / 64; ++i) {
+      ss += rs[i];
+      if (with_top) top.m = max(top.m, rt[i]);
+    }
+  }
+}
+
+template <class E, class U>
+__device__ __forceinline__ u32x2b_t eight8(const Eight<U>& e, const float h[8], const float w[8]) {
+  u32x2b_t r;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v |= ((uint32_t)e((U)h[4 * k + i] * (U)w[4 * k + i]) & 0xffu) << (8 * i);
+    r[k] = v;
+  }
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+// TPR threads a row (64: four rows a block of 256), NCH pieces of 8 elements a
+// thread; NCH 0: the row is swept twice, from memory.  MODE 0: the norm, 1: the norm
+// in 8 bits, 2: the quantiser alone.
+enum { NORM = 0, NORM8 = 1, QUANT = 2 };
+
+template <class E, int TPR, int NCH, int MODE, bool RES>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a) {
+  using S = typename E::S;
+  // the product h w of two 16-bit values is exact in fp32, that of fp32 values in fp64
+  using U = std::conditional_t<MODE == NORM8 && sizeof(S) == 4, double, float>;
+  constexpr int WPB = TPR == 64 ? 1 : TPR / 64;
+  __shared__ float rs[WPB];
+  __shared__ decltype(Top<U>::m) rt[WPB];
+  const int t = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
+  const int64_t row = TPR == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+  if (TPR == 64 && row >= a.rows) return;  // whole waves, and no barrier below
+  const S* x = (const S*)a.x + row * a.ldx;
+  const S* res = RES ? (const S*)a.res + row * a.ldres : nullptr;
+  S* hrow = RES ? (S*)a.h + row * a.ldh : nullptr;
+  const S* w = (const S*)a.w;
+  const int64_t cols = a.cols;
+  auto weight8 = [&](int64_t c, float v[8]) __attribute__((always_inline)) {
+    if (MODE == QUANT || !w) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 1.f;
+    } else {
+      E::expand(load_row8<E>(w, c, cols), v);
+    }
+  };
+  // h of a piece, written where the sum is kept
+  auto sum8 = [&](int64_t c) __attribute__((always_inline)) {
+    typename E::Raw r = load_row8<E>(x, c, cols);
+    if constexpr (RES) {
+      float v[8], u[8];
+      E::expand(r, v);
+      E::expand(load_row8<E>(res, c, cols), u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += u[k];
+      r = E::pack(v);
+      store_row8<E>(hrow, c, cols, r);
+    }
+    return r;
+  };
+  float ss = 0.f;
+  Top<U> top;
+  auto stats = [&](int64_t c, const typename E::Raw& r) __attribute__((always_inline)) {
+    float v[8];
+    E::expand(r, v);
+    if (MODE != QUANT) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ss += v[k] * v[k];
+    }
+    if (MODE != NORM) {
+      float f[8];
+      weight8(c, f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top.add((U)v[k] * (U)f[k]);
+    }
+  };
+  constexpr int N = NCH ? NCH : 1;
+  typename E::Raw held[N];
+  if constexpr (NCH) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * TPR + t);
+      if (c < cols) held[i] = sum8(c);
+    }
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * TPR + t);
+      if (c < cols) stats(c, held[i]);
+    }
+  } else {
+    for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, sum8(c));
+  }
+  row_reduce<TPR, U>(ss, top, MODE != NORM, rs, rt);
+  const float r = MODE == QUANT ? 1.f : 1.f / sqrtf(ss / (float)cols + a.eps);
+  const Eight<U> eight(top.value());
+  if (MODE != NORM && t == 0) a.scale[row] = eight.scale(r);
+  auto out = [&](int64_t c, const typename E::Raw& raw) __attribute__((always_inline)) {
+    float v[8], f[8];
+    E::expand(raw, v);
+    weight8(c, f);
+    if constexpr (MODE == NORM) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = v[k] * r * f[k];
+      store_row8<E>((S*)a.y + row * a.ldy, c, cols, E::pack(v));
+    } else {
+      store_q8(a.q + row * a.ldq, c, cols, eight8<E, U>(eight, v, f));
+    }
+  };
+  if constexpr (NCH) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * TPR + t);
+      if (c < cols) out(c, held[i]);
+    }
+  } else {
+    // the kept sum is read back by the thread that wrote it
+    for (int64_t c = 8 * t; c < cols; c += 8 * TPR) out(c, load_row8<E>(RES ? hrow : x, c, cols));
+  }
+}
+
+template <class E, int MODE, bool RES>
+hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
+  // a grid holds less than 2^32 threads: more rows go in slices
+  constexpr int64_t kSlice = 1 << 21;
+  if (a.rows > kSlice) {
+    NormArgs b = a;
+    for (int64_t r = 0; r < a.rows; r += kSlice) {
+      using S = typename E::S;
+      b.rows = a.rows - r < kSlice ? a.rows - r : kSlice;
+      b.x = (const S*)a.x + r * a.ldx;
+      if (RES) {
+        b.res = (const S*)a.res + r * a.ldres;
+        b.h = (S*)a.h + r * a.ldh;
+      }
+      if (MODE == NORM) {
+        b.y = (S*)a.y + r * a.ldy;
+      } else {
+        b.q = a.q + r * a.ldq;
+        b.scale = a.scale + r;
+      }
+      const hipError_t e = launch_rows<E, MODE, RES>(b, s);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+  if (a.rows == 0) return hipSuccess;
+  const int64_t pieces = (a.cols + 7) / 8;
+  const dim3 per_wave((unsigned)((a.rows + 3) / 4)), per_block((unsigned)a.rows);
+#define PRM_ROWS(TPR, NCH) rows_kernel<E, TPR, NCH, MODE, RES><<<TPR == 64 ? per_wave : per_block, TPR == 64 ? 256 : TPR, 0, s>>>(a)
+  if (pieces <= 64) PRM_ROWS(64, 1);
+  else if (a.rows >= 2048 && pieces <= 128) PRM_ROWS(64, 2);
+  else if (pieces <= 256) PRM_ROWS(256, 1);
+  else if (a.rows < 512 && pieces <= 1024) PRM_ROWS(1024, 1);
+  else if (pieces <= 512) PRM_ROWS(256, 2);
+  else if (pieces <= 1024) PRM_ROWS(256, 4);
+  else if (pieces <= 2048) PRM_ROWS(1024, 2);
+  else if (pieces <= 4096) PRM_ROWS(1024, 4);
+  else PRM_ROWS(1024, 0);
+#undef PRM_ROWS
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  if (a.y) return a.res ? launch_rows<E, NORM, true>(a, s) : launch_rows<E, NORM, false>(a, s);
+  return a.res ? launch_rows<E, NORM8, true>(a, s) : launch_rows<E, NORM8, false>(a, s);
+}
+
+// ---------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------
+// A row's threads keep their columns' share of dw over all the rows that they take
+// (row, row + step, ...), and leave it as one row of `part`; a second kernel adds those
+// rows in order.  NCH 0 (rows over 32768): two sweeps a row, and dw in `part` itself.
+template <class E, int TPR, int NCH>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGradArgs a) {
+  using S = typename E::S;
+  constexpr int WPB = TPR == 64 ? 1 : TPR / 64;
+  __shared__ float red[2][2][WPB];
+  const int t = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
+  const int part = TPR == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (part >= a.nparts) return;  // whole waves, and no barrier below (TPR 64)
+  const int64_t cols = a.cols;
+  const S* w = (const S*)a.w;
+  constexpr int N = NCH ? NCH : 1;
+  float dw[N][8];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[i][k] = 0.f;
+  auto weight8 = [&](int64_t c, float v[8]) __attribute__((always_inline)) {
+    if (w) E::expand(load_row8<E>(w, c, cols), v);
+    else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 1.f;
+    }
+  };
+  float* const mine = a.part + (int64_t)part * cols;
+  bool first = true;
+  int flip = 0;
+  for (int64_t row = part; row < a.rows; row += a.nparts) {
+    const S* gy = (const S*)a.gy + row * a.ldgy;
+    const S* h = (const S*)a.h + row * a.ldh;
+    const S* gh = a.gh ? (const S*)a.gh + row * a.ldgh : nullptr;
+    S* dx = (S*)a.dx + row * a.lddx;
+    typename E::Raw rh[N], rg[N];
+    float ss = 0.f, sg = 0.f;  // sums of h^2 and of g h
+    auto stats = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg) __attribute__((always_inline)) {
+      float v[8], g[8], f[8];
+      E::expand(xh, v);
+      E::expand(xg, g);
+      weight8(c, f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        ss += v[k] * v[k];
+        sg += g[k] * f[k] * v[k];
+      }
+    };
+    if constexpr (NCH) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * TPR + t);
+        if (c < cols) {
+          rh[i] = load_row8<E>(h, c, cols);
+          rg[i] = load_row8<E>(gy, c, cols);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * TPR + t);
+        if (c < cols) stats(c, rh[i], rg[i]);
+      }
+    } else {
+      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, load_row8<E>(h, c, cols), load_row8<E>(gy, c, cols));
+    }
+    ss = wave_sum(ss);
+    sg = wave_sum(sg);
+    if constexpr (TPR > 64) {
+      // two sets of slots in turn: a wave writes the next row's behind one barrier only
+      if ((threadIdx.x & 63) == 0) {
+        red[flip][0][threadIdx.x >> 6] = ss;
+        red[flip][1][threadIdx.x >> 6] = sg;
+      }
+      __syncthreads();
+      ss = sg = 0.f;
+#pragma unroll
+      for (int i = 0; i < WPB; ++i) {
+        ss += red[flip][0][i];
+        sg += red[flip][1][i];
+      }
+      flip ^= 1;
+    }
+    const float r = 1.f / sqrtf(ss / (float)cols + a.eps);
+    const float coef = r * r * (sg / (float)cols);  // mean(g n) r: what each h is scaled by
+    auto out = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, float d[8]) __attribute__((always_inline)) {
+      float v[8], g[8], f[8], o[8];
+      E::expand(xh, v);
+      E::expand(xg, g);
+      weight8(c, f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        d[k] += g[k] * (v[k] * r);
+        o[k] = r * (g[k] * f[k] - v[k] * coef);
+      }
+      if (gh) {
+        E::expand(load_row8<E>(gh, c, cols), v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] += v[k];
+      }
+      store_row8<E>(dx, c, cols, E::pack(o));
+    };
+    if constexpr (NCH) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * TPR + t);
+        if (c < cols) out(c, rh[i], rg[i], dw[i]);
+      }
+    } else {
+      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
+        float d[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[k] = first || c + k >= cols || !a.dw ? 0.f : mine[c + k];
+        out(c, load_row8<E>(h, c, cols), load_row8<E>(gy, c, cols), d);
+        if (a.dw)
+          for (int k = 0; k < 8 && c + k < cols; ++k) mine[c + k] = d[k];
+      }
+      first = false;
+    }
+  }
+  if (!a.dw) return;
+  if constexpr (NCH) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * TPR + t);
+      if (c >= cols) continue;
+      if (c + 8 <= cols) {
+        TF32::store8(mine + c, TF32::pack(dw[i]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + k < cols) mine[c + k] = dw[i][k];
+      }
+    }
+  }
+}
+
+// dw[c] = sum over parts, in order: 8 threads a column take each eighth part, and
+// their sums are added in order.
+template <class E>
+__global__ __launch_bounds__(256) void part_sum_kernel(const float* part, int nparts, int64_t cols, typename E::S* out) {
+  __shared__ float red[8][32];
+  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + tc;
+  float s = 0.f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = tr; i < nparts; i += 8) s += *gptr(part + (int64_t)i * cols + c);
+  }
+  red[tr][tc] = s;
+  __syncthreads();
+  if (tr == 0 && c < cols) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += red[i][tc];
+    E::store1(out + c, s);
+  }
+}
+
+template <class E>
+hipError_t launch_grad(const NormGradArgs& a, hipStream_t s) {
+  const int64_t pieces = (a.cols + 7) / 8;
+  if (a.rows > 0) {
+    const dim3 waves((unsigned)((a.nparts + 3) / 4)), blocks((unsigned)a.nparts);
+#define PRM_GRAD(TPR, NCH) norm_grad_kernel<E, TPR, NCH><<<TPR == 64 ? waves : blocks, TPR == 64 ? 256 : TPR, 0, s>>>(a)
+    if (pieces <= 64) PRM_GRAD(64, 1);
+    else if (pieces <= 256) PRM_GRAD(256, 1);
+    else if (pieces <= 512) PRM_GRAD(256, 2);
+    else if (pieces <= 1024) PRM_GRAD(1024, 1);
+    else if (pieces <= 2048) PRM_GRAD(1024, 2);
+    else if (pieces <= 4096) PRM_GRAD(1024, 4);
+    else PRM_GRAD(1024, 0);
+#undef PRM_GRAD
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dw)
+    part_sum_kernel<E><<<(unsigned)((a.cols + 31) / 32), 256, 0, s>>>(a.part, a.rows > 0 ? a.nparts : 0, a.cols, (typename E::S*)a.dw);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// quantiser of columns, transposed
+// ---------------------------------------------------------------------------
+// Largest magnitudes (as bits) and sums of the columns over a block of rows: 32 lanes
+// of 8 columns, 8 rows at a time.
+template <class E, bool SUM>
+__global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
+  using S = typename E::S;
+  __shared__ uint32_t rm[8][256];
+  __shared__ float rs[SUM ? 8 : 1][256];
+  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 256 + 8 * tc;
+  const int64_t r0 = (int64_t)blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  uint32_t m[8];
+  float sum[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) { m[k] = 0; sum[k] = 0.f; }
+  if (c < a.cols) {
+#pragma unroll 4
+    for (int64_t r = r0 + tr; r < r1; r += 8) {
+      float v[8];
+      E::expand(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols), v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        m[k] = max(m[k], __float_as_uint(v[k]) & 0x7fffffffu);
+        if (SUM) sum[k] += v[k];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    rm[tr][8 * tc + k] = m[k];
+    if (SUM) rs[tr][8 * tc + k] = sum[k];
+  }
+  __syncthreads();
+  const int64_t cc = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (cc >= a.cols) return;
+  uint32_t top = 0;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    top = max(top, rm[i][threadIdx.x]);
+    if (SUM) s += rs[i][threadIdx.x];
+  }
+  a.part_max[(int64_t)blockIdx.y * a.cols + cc] = top;
+  if (SUM) a.part_sum[(int64_t)blockIdx.y * a.cols + cc] = s;
+}
+
+// A tile of 128 rows x 64 columns: a thread quantises 4 rows of 8 columns, and the tile
+// leaves through shared memory as 128 bytes of each of its columns.
+template <class E, bool SUM>
+__global__ __launch_bounds__(256) void col_quant_kernel(QuantArgs a) {
+  using S = typename E::S;
+  constexpr int LD = 132;  // bytes of a column in shared memory: 33 banks
+  __shared__ uint32_t tile[64 * LD / 4];
+  __shared__ uint32_t pm[4][64];
+  __shared__ float ps[SUM ? 4 : 1][64];
+  __shared__ float tops[64];
+  const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
+  const bool first = blockIdx.y == 0;
+  {
+    const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
+    uint32_t m = 0;
+    float s = 0.f;
+    if (c0 + tc < a.cols) {
+      for (int i = tr; i < a.nrb; i += 4) {
+        m = max(m, *gptr(a.part_max + (int64_t)i * a.cols + c0 + tc));
+        if (SUM && first) s += *gptr(a.part_sum + (int64_t)i * a.cols + c0 + tc);
+      }
+    }
+    pm[tr][tc] = m;
+    if (SUM) ps[tr][tc] = s;
+    __syncthreads();
+    if (tr == 0) {
+      m = max(max(pm[0][tc], pm[1][tc]), max(pm[2][tc], pm[3][tc]));
+      tops[tc] = __uint_as_float(m);
+      if (first && c0 + tc < a.cols) {
+        a.scale[c0 + tc] = Eight<float>(__uint_as_float(m)).scale(1.f);
+        if (SUM) E::store1((S*)a.sum + c0 + tc, (ps[0][tc] + ps[1][tc]) + (ps[2][tc] + ps[3][tc]));
+      }
+    }
+    __syncthreads();
+  }
+  const int tc = threadIdx.x & 7, tr = threadIdx.x >> 3;
+  const int64_t c = c0 + 8 * tc;
+  float v[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = r0 + 4 * tr + i;
+    if (r < a.rows && c < a.cols) {
+      E::expand(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols), v[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const Eight<float> e(tops[8 * tc + k]);
+    uint32_t q = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q |= ((uint32_t)e(v[i][k]) & 0xffu) << (8 * i);
+    tile[(8 * tc + k) * (LD / 4) + tr] = q;
+  }
+  __syncthreads();
+  const int col = threadIdx.x >> 2, piece = threadIdx.x & 3;  // 32 bytes of a column each
+  if (c0 + col >= a.cols) return;
+  int8_t* out = a.q + (c0 + col) * a.ldq;
+  const uint32_t* src = tile + col * (LD / 4) + 8 * piece;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int64_t r = r0 + 32 * piece + 8 * k;
+    if (r < a.rows) store_q8(out, r, a.rows, u32x2b_t{src[2 * k], src[2 * k + 1]});
+  }
+}
+
+template <class E>
+hipError_t launch_cols(const QuantArgs& a, hipStream_t s) {
+  const dim3 g1((unsigned)((a.cols + 255) / 256), (unsigned)a.nrb);
+  const dim3 g2((unsigned)((a.cols + 63) / 64), (unsigned)((a.rows + 127) / 128));
+  if (a.sum) {
+    col_stats_kernel<E, true><<<g1, 256, 0, s>>>(a);
+    col_quant_kernel<E, true><<<g2, 256, 0, s>>>(a);
+  } else {
+    col_stats_kernel<E, false><<<g1, 256, 0, s>>>(a);
+    col_quant_kernel<E, false><<<g2, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(OpType t, const NormArgs& a, hipStream_t s) {
+  return t == OP_F32 ? launch_norm<TF32>(a, s) : t == OP_BF16 ? launch_norm<TBF16>(a, s) : launch_norm<TF16>(a, s);
+}
+
+hipError_t launch_quantize_rows(OpType t, const QuantArgs& q, hipStream_t s) {
+  NormArgs a = {};
+  a.x = q.x;
+  a.q = q.q;
+  a.scale = q.scale;
+  a.rows = q.rows;
+  a.cols = q.cols;
+  a.ldx = q.ldx;
+  a.ldq = q.ldq;
+  return t == OP_F32    ? launch_rows<TF32, QUANT, false>(a, s)
+         : t == OP_BF16 ? launch_rows<TBF16, QUANT, false>(a, s)
+                        : launch_rows<TF16, QUANT, false>(a, s);
+}
+
+// At most 64 row blocks of at least 64 rows each: the second kernel's blocks each read
+// them all.
+void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block) {
+  (void)cols;
+  int64_t per = (rows + 63) / 64;
+  per = per < 64 ? 64 : per;
+  *rows_per_block = (int32_t)per;
+  *nrb = (int32_t)((rows + per - 1) / per);
+}
+
+hipError_t launch_quantize_cols(OpType t, const QuantArgs& a, hipStream_t s) {
+  return t == OP_F32 ? launch_cols<TF32>(a, s) : t == OP_BF16 ? launch_cols<TBF16>(a, s) : launch_cols<TF16>(a, s);
+}
+
+// Rows of partial dw: one a block (a wave, for short rows), enough to fill the card and
+// few against the rows.
+int32_t rms_norm_grad_parts(int64_t rows, int64_t cols) {
+  const int64_t most = cols <= 512 ? 2048 : cols <= 4096 ? 1024 : 512;
+  return (int32_t)(rows < most ? (rows < 1 ? 1 : rows) : most);
+}
+
+hipError_t launch_rms_norm_grad(OpType t, const NormGradArgs& a, hipStream_t s) {
+  return t == OP_F32 ? launch_grad<TF32>(a, s) : t == OP_BF16 ? launch_grad<TBF16>(a, s) : launch_grad<TF16>(a, s);
+}
+
+}  // namespace prm

@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "../../include/prm.h"
+#include "ops_internal.h"
 #include "prm_internal.h"
 
 using namespace prm;
@@ -84,6 +85,16 @@ int check_device_ptr(int dev, const void* p, const char* what, int i, int k) {
                 a.device, dev);
   return fail(PRM_EINVAL, "%s %d: pointer %d is host memory; device memory is required", what, i, k);
 }
+
+}  // namespace
+
+// The operators' entry points (ops_api.hip) report as the step's do.
+namespace prm {
+int set_error(int code, const char* msg) { return fail(code, "%s", msg); }
+int device_pointer(int dev, const void* p, const char* what, int i, int k) { return check_device_ptr(dev, p, what, i, k); }
+}  // namespace prm
+
+namespace {
 
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline uint64_t align256(uint64_t x) { return (x + 255) & ~uint64_t(255); }

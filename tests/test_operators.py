@@ -1,0 +1,118 @@
+"""Refusals of the 8-bit linear layer's operators, on the CPU: every bad argument is
+turned down before a device is touched."""
+import ctypes
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2608_20818_amd as prm  # noqa: E402
+
+FAKE = 1 << 20  # never dereferenced: the arguments are refused first
+BF = prm.BF16
+
+
+def refused(name, args, code, word=""):
+    L = prm.load()
+    rc = getattr(L, name)(*args)
+    assert rc == code, (name, rc)
+    assert word in L.prm_last_error().decode(), L.prm_last_error()
+
+
+def changed(base, **kw):
+    out = dict(base)
+    out.update(kw)
+    return list(out.values())
+
+
+Q = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=8, scale=FAKE, stream=None)
+C = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=4, scale=FAKE, sum=None, ws=FAKE, nws=1 << 16, stream=None)
+M = dict(a=FAKE, lda=8, sa=FAKE, b=FAKE, ldb=8, sb=FAKE, bias=None, dtype=BF, out=FAKE, ldo=6, m=4, n=6, k=8, stream=None)
+N = dict(x=FAKE, ldx=8, res=None, ldres=0, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, h=None, ldh=0, y=FAKE, ldy=8, q=None,
+         ldq=0, scale=None, stream=None)
+G = dict(gy=FAKE, ldgy=8, gh=None, ldgh=0, h=FAKE, ldh=8, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, dx=FAKE, lddx=8,
+         dw=FAKE, ws=FAKE, nws=1 << 16, stream=None)
+BASE = {"prm_quantize_rows": Q, "prm_quantize_cols": C, "prm_int8_matmul": M, "prm_rms_norm": N, "prm_rms_norm_backward": G}
+
+
+@pytest.mark.parametrize("name", sorted(BASE))
+def test_unknown_type(name):
+    for t in (3, -1):
+        refused(name, changed(BASE[name], dtype=t), prm.PRM_EDTYPE, "dtype")
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("prm_quantize_rows", dict(rows=-1)), ("prm_quantize_rows", dict(cols=0)), ("prm_quantize_rows", dict(cols=(1 << 24) + 1)),
+    ("prm_quantize_rows", dict(rows=1 << 31)), ("prm_quantize_rows", dict(ldx=7)), ("prm_quantize_rows", dict(ldq=7)),
+    ("prm_quantize_rows", dict(x=None)), ("prm_quantize_rows", dict(q=None)), ("prm_quantize_rows", dict(scale=None)),
+    ("prm_quantize_cols", dict(rows=0)), ("prm_quantize_cols", dict(rows=(1 << 22) + 1, ldq=1 << 30)),
+    ("prm_quantize_cols", dict(ldq=3)), ("prm_quantize_cols", dict(ldx=7)), ("prm_quantize_cols", dict(nws=8)),
+    ("prm_quantize_cols", dict(ws=None)), ("prm_quantize_cols", dict(x=None)),
+    ("prm_int8_matmul", dict(k=0)), ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072)),
+    ("prm_int8_matmul", dict(m=-1)), ("prm_int8_matmul", dict(n=(1 << 24) + 1, ldo=1 << 30)),
+    ("prm_int8_matmul", dict(lda=7)), ("prm_int8_matmul", dict(ldb=7)), ("prm_int8_matmul", dict(ldo=5)),
+    ("prm_int8_matmul", dict(a=None)), ("prm_int8_matmul", dict(sb=None)), ("prm_int8_matmul", dict(out=None)),
+    ("prm_rms_norm", dict(eps=0.0)), ("prm_rms_norm", dict(eps=float("nan"))), ("prm_rms_norm", dict(eps=float("inf"))),
+    ("prm_rms_norm", dict(res=FAKE, ldres=8)), ("prm_rms_norm", dict(h=FAKE, ldh=8)),
+    ("prm_rms_norm", dict(res=FAKE, ldres=7, h=FAKE, ldh=8)), ("prm_rms_norm", dict(res=FAKE, ldres=8, h=FAKE, ldh=7)),
+    ("prm_rms_norm", dict(y=None)), ("prm_rms_norm", dict(q=FAKE, ldq=8)), ("prm_rms_norm", dict(y=None, q=FAKE, ldq=8)),
+    ("prm_rms_norm", dict(y=None, q=FAKE, ldq=7, scale=FAKE)), ("prm_rms_norm", dict(ldy=7)), ("prm_rms_norm", dict(cols=0)),
+    ("prm_rms_norm", dict(x=None)),
+    ("prm_rms_norm_backward", dict(eps=-1.0)), ("prm_rms_norm_backward", dict(ldgy=7)),
+    ("prm_rms_norm_backward", dict(gh=FAKE, ldgh=7)), ("prm_rms_norm_backward", dict(ldh=7)),
+    ("prm_rms_norm_backward", dict(lddx=7)), ("prm_rms_norm_backward", dict(nws=4)),
+    ("prm_rms_norm_backward", dict(ws=None)), ("prm_rms_norm_backward", dict(dx=None)),
+])
+def test_bad_argument(name, kw):
+    refused(name, changed(BASE[name], **kw), prm.PRM_EINVAL)
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("prm_quantize_rows", dict(x=FAKE + 1)), ("prm_quantize_rows", dict(scale=FAKE + 2)),
+    ("prm_quantize_rows", dict(x=FAKE + 2, dtype=prm.F32)), ("prm_quantize_cols", dict(ws=FAKE + 8)),
+    ("prm_int8_matmul", dict(out=FAKE + 1)), ("prm_int8_matmul", dict(sa=FAKE + 2)), ("prm_int8_matmul", dict(bias=FAKE + 1)),
+    ("prm_rms_norm", dict(w=FAKE + 1)), ("prm_rms_norm_backward", dict(gy=FAKE + 1)),
+])
+def test_off_an_elements_boundary(name, kw):
+    refused(name, changed(BASE[name], **kw), prm.PRM_EALIGN, "aligned")
+
+
+def test_nothing_to_do():
+    L = prm.load()
+    assert L.prm_quantize_rows(*changed(Q, rows=0, x=None, q=None, scale=None)) == prm.PRM_OK
+    assert L.prm_int8_matmul(*changed(M, m=0)) == prm.PRM_OK
+    assert L.prm_int8_matmul(*changed(M, n=0)) == prm.PRM_OK
+    assert L.prm_rms_norm(*changed(N, rows=0)) == prm.PRM_OK
+    assert L.prm_rms_norm_backward(*changed(G, rows=0, dw=None)) == prm.PRM_OK
+
+
+def test_workspace_sizes():
+    L = prm.load()
+    for f in (L.prm_quantize_cols_workspace, L.prm_rms_norm_backward_workspace):
+        assert f(0, 8) == 0 and f(8, 0) == 0 and f(8, (1 << 24) + 1) == 0
+        assert f(1, 1) > 0 and f(8192, 4096) >= 4 * 4096
+        assert f(8192, 4096) % 4 == 0
+    assert L.prm_quantize_cols_workspace((1 << 22) + 1, 8) == 0
+
+
+def test_the_step_takes_no_fp16():
+    with pytest.raises(prm.PRMError) as e:
+        prm.plan_workspace_bytes([(4, 8)], prm.config_default(param_dtype=prm.F16))
+    assert e.value.code == prm.PRM_EDTYPE
+
+
+def test_host_tensors_are_refused():
+    x, w = torch.zeros(3, 8), torch.zeros(5, 8)
+    q, s = torch.zeros(3, 8, dtype=torch.int8), torch.zeros(3)
+    for call in (lambda: prm.quantize_rows(x), lambda: prm.quantize_rows(x, transpose=True), lambda: prm.rms_norm(x),
+                 lambda: prm.int8_linear(x, w), lambda: prm.int8_matmul(q, s, q, s)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
+
+
+def test_names_are_public():
+    for n in ("quantize_rows", "int8_matmul", "int8_linear", "rms_norm"):
+        assert n in prm.__all__ and callable(getattr(prm, n))
+    assert ctypes.sizeof(ctypes.c_int32) == 4
