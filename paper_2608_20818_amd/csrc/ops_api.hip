@@ -136,9 +136,11 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   return launched(call, launch_quantize_cols((OpType)dtype, a, (hipStream_t)hip_stream));
 }
 
-int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
-                    const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m, int64_t n, int64_t k,
-                    void* hip_stream) {
+// prm_int8_matmul; `kind`: a ProductKind, or 0 for the rule's (tests hold every kernel to
+// the sizes that it takes).
+int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
+                             const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m,
+                             int64_t n, int64_t k, void* hip_stream, int32_t kind) {
   static const char* const call = "prm_int8_matmul";
   TRY(check_type(dtype));
   if (m < 0 || n < 0 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK)
@@ -151,7 +153,16 @@ int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const in
   TRY(check_buffers(call, {{a, "a", 1}, {a_scale, "a_scale", 4}, {b, "b", 1}, {b_scale, "b_scale", 4},
                            optional(bias, "bias", size_of(dtype)), {out, "out", size_of(dtype)}}));
   ProductArgs p = {a, b, a_scale, b_scale, bias, out, m, n, k, lda, ldb, ldo};
-  return launched(call, launch_int8_matmul((OpType)dtype, p, (hipStream_t)hip_stream));
+  if (kind < 0 || kind > PRODUCT_BIG || (kind && !product_takes(p, (ProductKind)kind)))
+    return fail(PRM_EINVAL, "%s: kernel %d does not take this product", call, kind);
+  const ProductKind kd = kind ? (ProductKind)kind : product_kind(p);
+  return launched(call, launch_int8_matmul((OpType)dtype, p, kd, (hipStream_t)hip_stream));
+}
+
+int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
+                    const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m, int64_t n, int64_t k,
+                    void* hip_stream) {
+  return prm_internal_int8_matmul(a, lda, a_scale, b, ldb, b_scale, bias, dtype, out, ldo, m, n, k, hip_stream, 0);
 }
 
 int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w, int32_t dtype,

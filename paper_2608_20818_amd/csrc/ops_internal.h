@@ -70,7 +70,10 @@ struct ProductArgs {
   void* out;         // m x n
   int64_t m, n, k, lda, ldb, ldo;
 };
-hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, hipStream_t s);
+enum ProductKind : int32_t { PRODUCT_FEW = 1, PRODUCT_SMALL = 2, PRODUCT_MID = 3, PRODUCT_BIG = 4 };
+bool product_takes(const ProductArgs& p, ProductKind kind);
+ProductKind product_kind(const ProductArgs& p);  // the rule
+hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, ProductKind kind, hipStream_t s);
 constexpr int64_t kMaxProductK = 131071;  // 128 * 128 * k stays below 2^31
 
 }  // namespace prm
