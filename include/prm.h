@@ -359,10 +359,16 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
  * (m x k: tokens), b (n x k: output channels, as a linear layer's weight is kept)
  * and out (m x n, type dtype).  The sum is exact (32-bit whole numbers: 1 <= k <=
  * 131071, where 128 * 128 k still fits), the rest fp32, rounded once.  bias: n values
- * of type dtype, or NULL.  0 <= m, n <= 2^24. */
+ * of type dtype, or NULL.  0 <= m, n <= 2^24.  Operands whose rows start on 16-byte
+ * boundaries (a and b, lda and ldb) take faster loads.  `workspace`:
+ * prm_int8_matmul_workspace(m, n, k) bytes (0 for most sizes), 16-byte aligned, used by
+ * this call only; a product with few outputs and a long sum is split there.  With less,
+ * or NULL, it is not split: the same result, later. */
+uint64_t prm_int8_matmul_workspace(int64_t m, int64_t n, int64_t k);
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
                     const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo,
-                    int64_t m, int64_t n, int64_t k, void* hip_stream);
+                    int64_t m, int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes,
+                    void* hip_stream);
 
 /* Root-mean-square norm of each row of x (rows x cols), after the residual's
  * addition where `residual` is not NULL:

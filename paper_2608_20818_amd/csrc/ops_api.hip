@@ -136,11 +136,12 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   return launched(call, launch_quantize_cols((OpType)dtype, a, (hipStream_t)hip_stream));
 }
 
-// prm_int8_matmul; `kind`: a ProductKind, or 0 for the rule's (tests hold every kernel to
-// the sizes that it takes).
+// prm_int8_matmul; `kind` and `splits`: a ProductPlan, or 0 for the rule's (tests hold
+// every kernel to the sizes that it takes).
 int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
                              const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m,
-                             int64_t n, int64_t k, void* hip_stream, int32_t kind) {
+                             int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes, void* hip_stream,
+                             int32_t kind, int32_t splits) {
   static const char* const call = "prm_int8_matmul";
   TRY(check_type(dtype));
   if (m < 0 || n < 0 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK)
@@ -150,19 +151,37 @@ int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale,
   TRY(check_ld(call, "ldb", ldb, k));
   TRY(check_ld(call, "ldo", ldo, n));
   if (m == 0 || n == 0) return PRM_OK;
+  ProductArgs p = {a, b, a_scale, b_scale, bias, out, m, n, k, lda, ldb, ldo, (int32_t*)workspace};
+  ProductPlan plan = {(ProductKind)kind, splits};
+  if (kind == 0) {
+    plan = product_plan(p);
+    // without the room that a split needs, the same sums in one piece
+    if (!workspace || workspace_bytes < product_workspace(m, n, plan.splits)) plan.splits = 1;
+  } else if (kind < 0 || kind >= PRODUCT_KINDS || !product_takes(p, plan)) {
+    return fail(PRM_EINVAL, "%s: kernel %d does not take this product in %d", call, kind, splits);
+  }
+  if (plan.splits > 1) TRY(check_workspace(call, workspace, workspace_bytes, product_workspace(m, n, plan.splits)));
   TRY(check_buffers(call, {{a, "a", 1}, {a_scale, "a_scale", 4}, {b, "b", 1}, {b_scale, "b_scale", 4},
-                           optional(bias, "bias", size_of(dtype)), {out, "out", size_of(dtype)}}));
-  ProductArgs p = {a, b, a_scale, b_scale, bias, out, m, n, k, lda, ldb, ldo};
-  if (kind < 0 || kind > PRODUCT_BIG || (kind && !product_takes(p, (ProductKind)kind)))
-    return fail(PRM_EINVAL, "%s: kernel %d does not take this product", call, kind);
-  const ProductKind kd = kind ? (ProductKind)kind : product_kind(p);
-  return launched(call, launch_int8_matmul((OpType)dtype, p, kd, (hipStream_t)hip_stream));
+                           optional(bias, "bias", size_of(dtype)), {out, "out", size_of(dtype)},
+                           optional(plan.splits > 1 ? workspace : nullptr, "workspace", 16)}));
+  return launched(call, launch_int8_matmul((OpType)dtype, p, plan, (hipStream_t)hip_stream));
+}
+
+uint64_t prm_int8_matmul_workspace(int64_t m, int64_t n, int64_t k) {
+  if (m < 1 || n < 1 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK) return 0;
+  ProductArgs p = {};
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  p.lda = p.ldb = (k + 15) / 16 * 16;
+  return product_workspace(m, n, product_plan(p).splits);
 }
 
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
                     const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m, int64_t n, int64_t k,
-                    void* hip_stream) {
-  return prm_internal_int8_matmul(a, lda, a_scale, b, ldb, b_scale, bias, dtype, out, ldo, m, n, k, hip_stream, 0);
+                    void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  return prm_internal_int8_matmul(a, lda, a_scale, b, ldb, b_scale, bias, dtype, out, ldo, m, n, k, workspace,
+                                  workspace_bytes, hip_stream, 0, 0);
 }
 
 int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w, int32_t dtype,

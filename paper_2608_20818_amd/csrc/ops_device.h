@@ -9,6 +9,7 @@ namespace prm {
 
 typedef unsigned u32x4e_t __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes, 2-byte alignment
 typedef unsigned u32x4b_t __attribute__((ext_vector_type(4), aligned(1)));   // 16 bytes, any alignment
+typedef unsigned u32x2e_t __attribute__((ext_vector_type(2), aligned(2)));   // 8 bytes, 2-byte alignment
 typedef unsigned u32x2b_t __attribute__((ext_vector_type(2), aligned(1)));   // 8 bytes, any alignment
 
 struct TF32 {
@@ -28,6 +29,7 @@ struct TF32 {
     *(PRM_GLOBAL f32x4u_t*)p = r.a;
     *(PRM_GLOBAL f32x4u_t*)(p + 4) = r.b;
   }
+  __device__ __forceinline__ static void store4(S* p, const float v[4]) { *(PRM_GLOBAL f32x4u_t*)p = f32x4u_t{v[0], v[1], v[2], v[3]}; }
   __device__ __forceinline__ static float load1(const S* p) { return *gptr(p); }
   __device__ __forceinline__ static void store1(S* p, float v) { *gptr(p) = v; }
 };
@@ -47,6 +49,9 @@ struct TBF16 {
     return Raw{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7])};
   }
   __device__ __forceinline__ static void store8(S* p, const Raw& r) { *(PRM_GLOBAL Raw*)p = r; }
+  __device__ __forceinline__ static void store4(S* p, const float v[4]) {
+    *(PRM_GLOBAL u32x2e_t*)p = u32x2e_t{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+  }
   __device__ __forceinline__ static float load1(const S* p) { return bf2f(*gptr(p)); }
   __device__ __forceinline__ static void store1(S* p, float v) { *gptr(p) = (uint16_t)f2bf(v); }
 };
@@ -71,6 +76,9 @@ struct TF16 {
     return r;
   }
   __device__ __forceinline__ static void store8(S* p, const Raw& r) { *(PRM_GLOBAL Raw*)p = r; }
+  __device__ __forceinline__ static void store4(S* p, const float v[4]) {
+    *(PRM_GLOBAL u32x2e_t*)p = u32x2e_t{down(v[0]) | (down(v[1]) << 16), down(v[2]) | (down(v[3]) << 16)};
+  }
   __device__ __forceinline__ static float load1(const S* p) { return up(*gptr(p)); }
   __device__ __forceinline__ static void store1(S* p, float v) { *gptr(p) = (uint16_t)down(v); }
 };

@@ -69,11 +69,22 @@ struct ProductArgs {
   const void* bias;  // n of the output's type, or nullptr
   void* out;         // m x n
   int64_t m, n, k, lda, ldb, ldo;
+  int32_t* part;     // the splits' sums, or nullptr
 };
-enum ProductKind : int32_t { PRODUCT_FEW = 1, PRODUCT_SMALL = 2, PRODUCT_MID = 3, PRODUCT_BIG = 4 };
-bool product_takes(const ProductArgs& p, ProductKind kind);
-ProductKind product_kind(const ProductArgs& p);  // the rule
-hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, ProductKind kind, hipStream_t s);
+// The kernels, by tile; ANY: rows that start on any byte.  The piped ones (64, 128) can
+// split k over blocks, whose sums meet in `part` (product_workspace bytes).
+enum ProductKind : int32_t {
+  PRODUCT_FEW = 1, PRODUCT_ANY64, PRODUCT_ANY128, PRODUCT_64, PRODUCT_128, PRODUCT_128_PAIRED, PRODUCT_256,
+  PRODUCT_KINDS
+};
+struct ProductPlan {
+  ProductKind kind;
+  int32_t splits;
+};
+bool product_takes(const ProductArgs& p, const ProductPlan& plan);
+ProductPlan product_plan(const ProductArgs& p);  // the rule
+uint64_t product_workspace(int64_t m, int64_t n, int32_t splits);
+hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, const ProductPlan& plan, hipStream_t s);
 constexpr int64_t kMaxProductK = 131071;  // 128 * 128 * k stays below 2^31
 
 }  // namespace prm

@@ -158,9 +158,12 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
         bm, ldb = _rows(b)
         sa, sb = a_scale.contiguous(), b_scale.contiguous()
         bv = None if bias is None else _vector(bias.detach())
-        _check(load().prm_int8_matmul(m.data_ptr(), lda, sa.data_ptr(), bm.data_ptr(), ldb, sb.data_ptr(),
-                                      None if bv is None else bv.data_ptr(), _CODE[dtype], out.data_ptr(), max(n, 1),
-                                      rows, n, k, stream))
+        L = load()
+        need = L.prm_int8_matmul_workspace(rows, n, k)
+        ws = torch.empty(need, dtype=torch.uint8, device=a.device) if need else None
+        _check(L.prm_int8_matmul(m.data_ptr(), lda, sa.data_ptr(), bm.data_ptr(), ldb, sb.data_ptr(),
+                                 None if bv is None else bv.data_ptr(), _CODE[dtype], out.data_ptr(), max(n, 1),
+                                 rows, n, k, ws.data_ptr() if need else None, need, stream))
     return out
 
 

@@ -15,6 +15,7 @@ range's fixed step):
   r (|g| + |n| mean|g n|) + |gh|; dw: (S / 2 + 4 + 2) u for each term, and the additions:
   rows / parts + parts / 8 + 16, with parts of at least 1 and at most 2048 rows.
 """
+import ctypes
 import os
 import sys
 
@@ -263,6 +264,55 @@ def test_product_strides(m):
     check_product(got, a, sa, b, sb, None, t)
 
 
+# kernels by number (1: few tokens, 2 and 3: rows on any byte, tiles of 64 and 128, 4 to 6: 64,
+# 128, 128 with two buffers, 7: 256), and in how many pieces k is split
+KERNELS = [(1, 1), (2, 1), (3, 1), (4, 1), (5, 1), (6, 1), (7, 1), (4, 2), (4, 7), (5, 3), (6, 2)]
+SIZES = [(1, 1, 1), (3, 65, 515), (16, 100, 3000), (65, 64, 16), (70, 50, 128), (129, 257, 400), (300, 300, 1000), (257, 511, 1072), (513, 130, 1152),
+         (64, 70, 8192), (520, 900, 2053)]
+
+
+@pytest.mark.parametrize("kernel", KERNELS, ids=str)
+def test_every_kernel(kernel):
+    # every kernel at every size that it takes, whatever the rule would choose
+    kind, splits = kernel
+    P, i64, i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+    f = prm.load().prm_internal_int8_matmul
+    f.argtypes = [P, i64, P, P, i64, P, P, i32, P, i64, i64, i64, i64, P, ctypes.c_uint64, P, i32, i32]
+    ran = 0
+    for m, n, k in SIZES:
+        ld = (k + 15) // 16 * 16 if kind > 3 else k + k % 2
+        a, b, sa, sb, t = int8s((m, k), 22), int8s((n, k), 23), scales(m, 24), scales(n, 25), torch.float32
+        ag, bg = on_gpu(a, ld, 0), on_gpu(b, ld, 0)
+        bias = rand((n,), t, 26)
+        ws = torch.empty(splits * m * (n + 7) * 4, dtype=torch.uint8, device="cuda")
+        out = torch.full((m + 1, n + 3), 7.0, device="cuda")
+        sag, sbg, biasg = sa.cuda(), sb.cuda(), bias.cuda()
+        rc = f(ag.data_ptr(), ld, sag.data_ptr(), bg.data_ptr(), ld, sbg.data_ptr(), biasg.data_ptr(), prm.F32, out.data_ptr(), n + 3, m, n, k,
+               ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream, kind, splits)
+        if rc == prm.PRM_EINVAL and (kind == 1 and m > 16 or splits > k // 128):
+            continue
+        assert rc == prm.PRM_OK, prm.load().prm_last_error()
+        ran += 1
+        check_product(out[:m, :n], a, sa, b, sb, bias, t)
+        out[:m, :n] = 7
+        assert (out == 7).all()
+    assert ran >= 3
+
+
+def test_product_without_its_workspace():
+    m, n, k = 40, 200, 16000
+    a, b, sa, sb = int8s((m, k), 27).cuda(), int8s((n, k), 28).cuda(), scales(m, 29).cuda(), scales(n, 30).cuda()
+    L = prm.load()
+    assert L.prm_int8_matmul_workspace(m, n, k) > 0 and L.prm_int8_matmul_workspace(4096, 4096, 4096) == 0
+    want = prm.int8_matmul(a, sa, b, sb, dtype=torch.float32)
+    got = torch.empty_like(want)
+    for ws, need in ((None, 0), (torch.empty(16, dtype=torch.uint8, device="cuda"), 16)):
+        got.zero_()
+        assert L.prm_int8_matmul(a.data_ptr(), k, sa.data_ptr(), b.data_ptr(), k, sb.data_ptr(), None, prm.F32, got.data_ptr(), n, m, n, k,
+                                 None if ws is None else ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == prm.PRM_OK
+        assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("m,k", [(1, 131071), (64, 131071), (70, 131071), (300, 131071)])
 def test_product_longest_sum(m, k):
     # every term as large as it can be: the sum comes within 2^14 of 2^31
@@ -282,7 +332,7 @@ def test_product_leaves_what_is_around():
     for mm in (5, 70):
         out = torch.full((mm + 2, 48), 7.0, device="cuda")
         assert L.prm_int8_matmul(ag.data_ptr(), k, sag.data_ptr(), bg.data_ptr(), k, sbg.data_ptr(), None, prm.F32, out[1].data_ptr() + 4,
-                                 48, mm, n, k, st) == prm.PRM_OK
+                                 48, mm, n, k, None, 0, st) == prm.PRM_OK
         check_product(out[1:mm + 1, 1:n + 1], a[:mm], sa[:mm], b, sb, None, torch.float32)
         out[1:mm + 1, 1:n + 1] = 7
         assert (out == 7).all()

@@ -29,7 +29,7 @@ def changed(base, **kw):
 
 Q = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=8, scale=FAKE, stream=None)
 C = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=4, scale=FAKE, sum=None, ws=FAKE, nws=1 << 16, stream=None)
-M = dict(a=FAKE, lda=8, sa=FAKE, b=FAKE, ldb=8, sb=FAKE, bias=None, dtype=BF, out=FAKE, ldo=6, m=4, n=6, k=8, stream=None)
+M = dict(a=FAKE, lda=8, sa=FAKE, b=FAKE, ldb=8, sb=FAKE, bias=None, dtype=BF, out=FAKE, ldo=6, m=4, n=6, k=8, ws=None, nws=0, stream=None)
 N = dict(x=FAKE, ldx=8, res=None, ldres=0, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, h=None, ldh=0, y=FAKE, ldy=8, q=None,
          ldq=0, scale=None, stream=None)
 G = dict(gy=FAKE, ldgy=8, gh=None, ldgh=0, h=FAKE, ldh=8, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, dx=FAKE, lddx=8,
