@@ -92,11 +92,11 @@ def copy_probe():
 
 
 def kernel_source_hash() -> str:
-    """Of the optimizer step's sources in libprm (not the Python binding's own checks,
-    marshal.cpp, nor the operators beside the step, ops_*)."""
+    """Of the optimizer step's sources in libprm (not the Python binding's own, marshal.cpp
+    and operators.cpp, nor the operators beside the step, ops_*)."""
     import hashlib
     d = os.path.join(ROOT, "paper_2608_20818_amd", "csrc")
-    src = b"".join(open(os.path.join(d, n), "rb").read() for n in sorted(os.listdir(d)) if n != "marshal.cpp" and not n.startswith("ops_"))
+    src = b"".join(open(os.path.join(d, n), "rb").read() for n in sorted(os.listdir(d)) if not n.endswith(".cpp") and not n.startswith("ops_"))
     return hashlib.sha256(src).hexdigest()[:16]
 
 

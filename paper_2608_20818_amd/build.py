@@ -75,37 +75,56 @@ def build(verbose: bool = False) -> str:
 
 MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")
 MARSHAL_LIB = os.path.join(HERE, "_marshal.so")
+OPERATORS_SRC = os.path.join(CSRC, "operators.cpp")
+OPERATORS_LIB = os.path.join(HERE, "_operators.so")
 
 
-def build_marshal() -> str:
-    """The binding's native tensor checks (g++, torch's C++ headers, no device
-    code): csrc/marshal.cpp -> _marshal.so, a CPython module.  The library and the
-    binding work without it (the checks then run in Python), so where torch, its
-    headers or Python's are missing nothing is built and "" returned."""
+def _build_binding(src: str, lib: str, flags=(), libs=(), needs=()) -> str:
+    """A part of the binding in native code (g++, torch's C++ headers, no device code):
+    ``src`` -> ``lib``, a CPython module.  The library and the binding work without
+    it (its work is then done in Python), so where torch, its headers or Python's
+    are missing nothing is built and "" returned."""
     import sysconfig
 
+    name = os.path.basename(lib)
     try:
         import torch
     except ImportError:
-        print("_marshal.so not built: no torch", file=sys.stderr)
+        print(f"{name} not built: no torch", file=sys.stderr)
         return ""
     root = os.path.dirname(torch.__file__)
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
            sysconfig.get_paths()["include"]]
-    for need in (os.path.join(inc[0], "torch", "csrc", "autograd", "python_variable.h"), os.path.join(inc[2], "Python.h")):
+    for need in (os.path.join(inc[0], "torch", "csrc", "autograd", "python_variable.h"), os.path.join(inc[2], "Python.h"),
+                 *[os.path.join(inc[0], n) for n in needs]):
         if not os.path.exists(need):
-            print(f"_marshal.so not built: no {need}", file=sys.stderr)
+            print(f"{name} not built: no {need}", file=sys.stderr)
             return ""
-    tmp = MARSHAL_LIB + ".tmp"
+    tmp = lib + ".tmp"
     cmd = [shutil.which("g++") or "g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *[f"-I{i}" for i in inc], MARSHAL_SRC,
-           "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *[f"-I{i}" for i in inc], *flags, src,
+           "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", *libs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         print(r.stdout, r.stderr, file=sys.stderr)
-        raise RuntimeError("g++ failed for csrc/marshal.cpp")
-    os.replace(tmp, MARSHAL_LIB)
-    return MARSHAL_LIB
+        raise RuntimeError(f"g++ failed for csrc/{os.path.basename(src)}")
+    os.replace(tmp, lib)
+    return lib
+
+
+def build_marshal() -> str:
+    """The native tensor checks of a step: csrc/marshal.cpp -> _marshal.so."""
+    return _build_binding(MARSHAL_SRC, MARSHAL_LIB)
+
+
+def build_operators() -> str:
+    """The operators' native calls: csrc/operators.cpp -> _operators.so, linked to
+    libprm.so (which is built first)."""
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    return _build_binding(OPERATORS_SRC, OPERATORS_LIB,
+                          flags=["-D__HIP_PLATFORM_AMD__", "-I", os.path.join(rocm, "include")],
+                          libs=["-lc10_hip", "-L", HERE, "-lprm", "-Wl,-rpath,$ORIGIN"],
+                          needs=[os.path.join("c10", "hip", "HIPStream.h")])
 
 
 C_CALLER_SRC = os.path.join(ROOT, "tests", "c_caller.c")
@@ -134,4 +153,5 @@ def build_c_caller() -> str:
 if __name__ == "__main__":
     print(build(verbose="-v" in sys.argv))
     print(build_marshal())
+    print(build_operators())
     print(build_c_caller())

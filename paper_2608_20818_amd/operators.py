@@ -17,6 +17,14 @@ import torch
 
 from . import BF16, F16, F32, _check, load
 
+load()  # libprm.so, or a loud error
+try:  # the plain calls, natively where _operators.so is built; None: not a plain call
+    from . import _operators as _native
+except ImportError:
+    class _native:
+        quantize_rows = quantize_cols = int8_matmul = staticmethod(lambda *a: None)
+        rms_norm = rms_norm_backward = linear_forward = linear_backward = staticmethod(lambda *a: None)
+
 __all__ = ["quantize_rows", "int8_matmul", "int8_linear", "rms_norm"]
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -97,11 +105,14 @@ def quantize_rows(x, transpose: bool = False):
     (``scale`` has the leading dimensions).  ``transpose`` (2-D ``x`` only): the columns
     instead, ``q`` is ``[cols, rows]`` and ``scale`` ``[cols]``, what
     ``quantize_rows(x.t())`` gives without a transposed copy.  Not differentiable."""
+    if transpose:
+        return _quantize_cols(x, False)[:2]
+    r = _native.quantize_rows(x)
+    if r is not None:
+        return r if type(r) is tuple else _check(r)
     _on_device(x, "x")
     code = _float_code(x, "x")
     x = x.detach()
-    if transpose:
-        return _quantize_cols(x, code, False)[:2]
     rows, cols = _count(x)
     with _device_of(x) as stream:
         q, ldq = _eight_bits(x.shape[:-1], cols, x.device)
@@ -111,7 +122,13 @@ def quantize_rows(x, transpose: bool = False):
     return q, scale
 
 
-def _quantize_cols(x, code, with_sum):
+def _quantize_cols(x, with_sum):
+    r = _native.quantize_cols(x, with_sum)
+    if r is not None:
+        return r if type(r) is tuple else _check(r)
+    _on_device(x, "x")
+    code = _float_code(x, "x")
+    x = x.detach()
     if x.dim() != 2:
         raise ValueError(f"x: the transposed form needs a matrix, got {tuple(x.shape)}")
     rows, cols = _count(x)
@@ -135,6 +152,9 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 131071) is exact;
     scales and bias are applied in fp32 and the result rounded once.  Not
     differentiable (``int8_linear`` is)."""
+    r = _native.int8_matmul(a, a_scale, b, b_scale, bias, _CODE.get(dtype, -1))
+    if r is not None:
+        return _check(r) if type(r) is int else r
     for t, what in ((a, "a"), (b, "b")):
         _on_device(t, what)
         if t.dtype != torch.int8:
@@ -198,7 +218,11 @@ def _norm(x, weight, residual, eps, quantize):
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
-        y, _, _, h = _norm(x, weight, residual, eps, False)
+        r = _native.rms_norm(x, weight, residual, eps, False, True)
+        if r is None:
+            y, _, _, h = _norm(x, weight, residual, eps, False)
+        else:
+            y, h = (_check(r) if type(r) is int else r) if residual is not None else (r if type(r) is not int else _check(r), None)
         ctx.save_for_backward(x if h is None else h, weight)
         ctx.eps = eps
         ctx.set_materialize_grads(False)
@@ -212,6 +236,10 @@ class _RmsNorm(torch.autograd.Function):
         if gy is None:  # only the kept sum has a gradient
             dw = torch.zeros_like(weight) if need_dw else None
             return (gh if ctx.needs_input_grad[0] else None), dw, (gh if ctx.needs_input_grad[2] else None), None
+        r = _native.rms_norm_backward(gy, gh, h, weight, ctx.eps, need_dw)
+        if r is not None:
+            dx, dw = r if type(r) is tuple else _check(r)
+            return (dx if ctx.needs_input_grad[0] else None), dw, (dx if ctx.needs_input_grad[2] else None), None
         rows, cols = _count(h)
         L = load()
         with _device_of(h) as stream:
@@ -238,6 +266,10 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
     ``(q, scale)`` or ``(q, scale, h)``, for ``int8_matmul``.  ``weight`` ``[cols]`` and
     ``residual`` (shaped as x) have x's type.  The plain outputs are differentiable in
     x, weight and residual; the 8-bit ones are not."""
+    eps = float(eps)
+    r = _native.rms_norm(x, weight, residual, eps, quantize, False)
+    if r is not None:
+        return _check(r) if type(r) is int else r
     _on_device(x, "x")
     _float_code(x, "x")
     _, cols = _count(x)
@@ -245,7 +277,6 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
         _same(residual, x, x.shape, "residual")
     if weight is not None:
         _same(weight, x, (cols,), "weight")
-    eps = float(eps)
     grad = torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
                                         or (residual is not None and residual.requires_grad))
     if quantize:
@@ -260,33 +291,41 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
 
 
 # ---- linear layer ------------------------------------------------------------
+def _linear(x, weight, bias):
+    r = _native.linear_forward(x, weight, bias)
+    if r is not None:
+        return _check(r) if type(r) is int else r
+    return int8_matmul(*quantize_rows(x), *quantize_rows(weight), bias=bias, dtype=x.dtype)
+
+
 class _Int8Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias):
         ctx.save_for_backward(x, weight)
-        ctx.with_bias = bias is not None
-        return int8_matmul(*quantize_rows(x), *quantize_rows(weight), bias=bias, dtype=x.dtype)
+        return _linear(x, weight, bias)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, gy):
         x, weight = ctx.saved_tensors
         need_x, need_w, need_b = ctx.needs_input_grad
+        r = _native.linear_backward(gy, x, weight, need_x, need_w, need_b)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
         g = gy.reshape(-1, gy.shape[-1])
         dx = dw = db = None
         if g.shape[0] == 0:
             return (torch.zeros_like(x) if need_x else None, torch.zeros_like(weight) if need_w else None,
                     weight.new_zeros(weight.shape[0]) if need_b else None)
-        code = _CODE[x.dtype]
         if need_x:
-            wq, ws, _ = _quantize_cols(weight, code, False)
+            wq, ws, _ = _quantize_cols(weight, False)
             dx = int8_matmul(*quantize_rows(g), wq, ws, dtype=x.dtype).reshape(x.shape)
         if need_w:
-            gq, gs, db = _quantize_cols(g, code, need_b)
-            xq, xs, _ = _quantize_cols(x.reshape(-1, x.shape[-1]), code, False)
+            gq, gs, db = _quantize_cols(g, need_b)
+            xq, xs, _ = _quantize_cols(x.reshape(-1, x.shape[-1]), False)
             dw = int8_matmul(gq, gs, xq, xs, dtype=x.dtype)
         elif need_b:
-            db = _quantize_cols(g, code, True)[2]
+            db = _quantize_cols(g, True)[2]
         return dx, dw, db
 
 
