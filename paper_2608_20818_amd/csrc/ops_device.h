@@ -2,6 +2,8 @@
 // start on any element, and the 8-bit rounding.
 #pragma once
 
+#include <type_traits>
+
 #include "ops_internal.h"
 #include "prm_device.h"
 
@@ -115,50 +117,84 @@ __device__ __forceinline__ void store_q8(int8_t* row, int64_t c, int64_t cols, c
 }
 
 // ---- 8 bits ----------------------------------------------------------------------
-// q = the whole number nearest to 127 u / top, ties to even, decided exactly: in fp32
-// where the quotient lies clear of a border of two whole numbers, and otherwise (about
-// one value in 5000) by comparing 254 |u| with (2 k + 1) top in fp64, which holds both
-// (fp32 products u: to its last bit).  The fp32 quotient is off by at most five
-// roundings of 2^-24, 127 * 5 * 2^-24 = 3.8e-5, so 1e-4 is clear.  u and top are first
-// scaled by a power of two that brings top near 1: no row is too small or too large.
-__device__ __forceinline__ int ilogb_(float t) { return __builtin_amdgcn_frexp_expf(t); }
-__device__ __forceinline__ int ilogb_(double t) { return __builtin_amdgcn_frexp_exp(t); }
-
-template <typename U>
+// q = the whole number nearest to 127 u / top, ties to even, decided exactly.  In fp32,
+// adding 1.5 * 2^23 to u inv (inv = 127 / top) rounds it to a whole number, which the
+// sum's low byte holds; what is left over says how far from the border of two whole
+// numbers it fell.  inv is off by 2 * 2^-24 at most, and u by 2^-24 (fp32 products: none):
+// 127 * 3 * 2^-24 = 2.3e-5, so where the remainder stays 3e-5 clear of 1/2 the number is
+// right.  Otherwise (in 1 of 2000 groups of 8) fp64 decides by comparing 254 |u| with
+// (2 k + 1) top, which it holds exactly (products of fp32 values: to its last bit).  Rows
+// too small or too large for fp32 are left to fp64 as a whole.  Five instructions a
+// value; checking each value apart took twelve, and bound the quantisers.
+template <typename U, bool EXACT32>
 struct Eight {
-  U top;      // max |u| of the row; 0, or not finite: every q is 0
-  U pw;       // the power of two
-  float inv;  // 127 / (top pw)
-  bool some;
+  using X = std::conditional_t<EXACT32, float, double>;
+  U top;      // max |u| of the row
+  float inv;  // 0: every q is 0 (a row of zeros, or one with a value that is not finite)
+  bool fp32;  // fp32 decides where it can
+  __device__ __forceinline__ Eight() {}
   __device__ __forceinline__ explicit Eight(U t) : top(t) {
-    some = t > (U)0 && finite();
-    int e = 0;
-    if constexpr (sizeof(U) == 8) {
-      e = some ? ilogb_(t) : 0;
-      pw = __builtin_ldexp(1.0, -e);
-    } else {
-      e = some ? ilogb_(t) : 0;
-      pw = __builtin_ldexpf(1.f, min(max(-e, -126), 120));
-    }
-    inv = some ? 127.f / (float)(t * pw) : 0.f;
+    fp32 = t > (U)1e-35f && t < (U)3e38f;
+    inv = fp32 ? 127.f / (float)t : 0.f;
   }
   __device__ __forceinline__ bool finite() const { return top < (U)__builtin_huge_valf(); }
-  __device__ __forceinline__ float quotient(U u) const { return some ? (float)(u * pw) * inv : 0.f; }
-  __device__ __forceinline__ static bool close(float f) { return fabsf(fabsf(f - rintf(f)) - 0.5f) < 1e-4f; }
-  __device__ __forceinline__ int decide(U u, float f) const {
-    const int k = (int)floorf(fabsf(f));
-    const double l = 254.0 * fabs((double)u), r = (2 * k + 1) * (double)top;
+  __device__ __forceinline__ int whole(U u, int k) const {  // k or k + 1 of |u|
+    return side((X)254 * (X)(u < 0 ? -u : u), (X)(2 * k + 1) * (X)top, u, k);
+  }
+  template <typename Y>
+  __device__ __forceinline__ static int side(Y l, Y r, U u, int k) {
     const int q = l > r ? k + 1 : l < r ? k : k + (k & 1);
-    return f < 0.f ? -q : q;
+    return u < 0 ? -q : q;
   }
-  __device__ __forceinline__ int operator()(U u) const {
-    const float f = quotient(u);
-    return close(f) ? decide(u, f) : (int)rintf(f);
+  // the floor of the quotient; next to a whole number it may be the one below: the same q
+  __device__ __forceinline__ int exactly(U u) const {
+    if (fp32) return whole(u, (int)floorf(fabsf((float)u * inv)));
+    if (!(top > (U)0) || !finite()) return 0;
+    const int k = (int)floor(127.0 * (fabs((double)u) / (double)top));
+    return side(254.0 * fabs((double)u), (2 * k + 1) * (double)top, u, k);
   }
+  // q of one value in the low byte; `rest`: the largest |remainder| so far
+  __device__ __forceinline__ uint32_t fast(U u, float& rest) const {
+    constexpr float kMagic = 12582912.f;
+    const float n = fmaf((float)u, inv, kMagic);
+    rest = fmaxf(rest, fabsf(fmaf((float)u, inv, kMagic - n)));
+    return __float_as_uint(n);
+  }
+  __device__ __forceinline__ bool sure(float rest) const { return fp32 && rest < 0.49997f; }
   // the scale: factor * top / 127; a row with a value that is not finite has NaN
   __device__ __forceinline__ float scale(float factor) const {
     return finite() ? (float)((double)factor * (double)top / 127.0) : __builtin_nanf("");
   }
+};
+// the low bytes of four words
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+// Largest magnitude, as the bits of a float, that keeps a NaN: of 16-bit values two at a
+// time on their bits as stored (NaN above infinity above the finite ones).
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+template <class E> struct TopRaw {
+  u16x2_t m = {0, 0};
+  __device__ __forceinline__ void add(const typename E::Raw& r) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, r[k] & 0x7fff7fffu));
+  }
+  __device__ __forceinline__ uint32_t bits() const {
+    const uint16_t h = m[0] > m[1] ? m[0] : m[1];
+    float v[8];
+    typename E::Raw r = {h, 0u, 0u, 0u};
+    E::expand(r, v);
+    return __float_as_uint(v[0]);
+  }
+};
+template <> struct TopRaw<TF32> {
+  uint32_t m = 0;
+  __device__ __forceinline__ void add(const TF32::Raw& r) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = max(max(m, __float_as_uint(r.a[k]) & 0x7fffffffu), __float_as_uint(r.b[k]) & 0x7fffffffu);
+  }
+  __device__ __forceinline__ uint32_t bits() const { return m; }
 };
 
 }  // namespace prm

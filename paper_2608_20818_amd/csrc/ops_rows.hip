@@ -45,8 +45,8 @@ template <> struct Top<double> {
 
 // Sum, and largest, over the threads of a row: a wave, or the whole block.
 template <int TPR, typename U>
-__device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_top, float* rs, decltype(Top<U>::m)* rt) {
-  ss = wave_sum(ss);
+__device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_sum, bool with_top, float* rs, decltype(Top<U>::m)* rt) {
+  if (with_sum) ss = wave_sum(ss);
   if (with_top) top.m = wave_max(top.m);
   if constexpr (TPR > 64) {
     const int w = threadIdx.x >> 6;
@@ -64,17 +64,17 @@ __device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_top
   }
 }
 
-template <class E, class U>
-__device__ __forceinline__ u32x2b_t eight8(const Eight<U>& e, const float h[8], const float w[8]) {
-  u32x2b_t r;
+template <class U, bool X>
+__device__ __forceinline__ u32x2b_t eight8(const Eight<U, X>& e, const U u[8]) {
+  uint32_t n[8];
+  float rest = 0.f;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    uint32_t v = 0;
+  for (int k = 0; k < 8; ++k) n[k] = e.fast(u[k], rest);
+  if (!e.sure(rest)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v |= ((uint32_t)e((U)h[4 * k + i] * (U)w[4 * k + i]) & 0xffu) << (8 * i);
-    r[k] = v;
+    for (int k = 0; k < 8; ++k) n[k] = (uint32_t)e.exactly(u[k]);
   }
-  return r;
+  return u32x2b_t{low_bytes(n[0], n[1], n[2], n[3]), low_bytes(n[4], n[5], n[6], n[7])};
 }
 
 // ---------------------------------------------------------------------------
@@ -125,19 +125,21 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a)
   };
   float ss = 0.f;
   Top<U> top;
+  TopRaw<E> raw_top;
   auto stats = [&](int64_t c, const typename E::Raw& r) __attribute__((always_inline)) {
     float v[8];
-    E::expand(r, v);
     if (MODE != QUANT) {
+      E::expand(r, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) ss += v[k] * v[k];
     }
-    if (MODE != NORM) {
+    if (MODE == NORM8) {
       float f[8];
       weight8(c, f);
 #pragma unroll
       for (int k = 0; k < 8; ++k) top.add((U)v[k] * (U)f[k]);
     }
+    if (MODE == QUANT) raw_top.add(r);
   };
   constexpr int N = NCH ? NCH : 1;
   typename E::Raw held[N];
@@ -155,9 +157,10 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a)
   } else {
     for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, sum8(c));
   }
-  row_reduce<TPR, U>(ss, top, MODE != NORM, rs, rt);
+  if constexpr (MODE == QUANT) top.m = raw_top.bits();
+  row_reduce<TPR, U>(ss, top, MODE != QUANT, MODE != NORM, rs, rt);
   const float r = MODE == QUANT ? 1.f : 1.f / sqrtf(ss / (float)cols + a.eps);
-  const Eight<U> eight(top.value());
+  const Eight<U, sizeof(S) == 2 && (MODE == QUANT || std::is_same_v<E, TBF16>)> eight(top.value());
   if (MODE != NORM && t == 0) a.scale[row] = eight.scale(r);
   auto out = [&](int64_t c, const typename E::Raw& raw) __attribute__((always_inline)) {
     float v[8], f[8];
@@ -168,7 +171,10 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a)
       for (int k = 0; k < 8; ++k) v[k] = v[k] * r * f[k];
       store_row8<E>((S*)a.y + row * a.ldy, c, cols, E::pack(v));
     } else {
-      store_q8(a.q + row * a.ldq, c, cols, eight8<E, U>(eight, v, f));
+      U u[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] = (U)v[k] * (U)f[k];
+      store_q8(a.q + row * a.ldq, c, cols, eight8(eight, u));
     }
   };
   if constexpr (NCH) {
@@ -431,16 +437,24 @@ __global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) { m[k] = 0; sum[k] = 0.f; }
   if (c < a.cols) {
-#pragma unroll 4
-    for (int64_t r = r0 + tr; r < r1; r += 8) {
+    const auto add = [&](const typename E::Raw& raw) __attribute__((always_inline)) {
       float v[8];
-      E::expand(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols), v);
+      E::expand(raw, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         m[k] = max(m[k], __float_as_uint(v[k]) & 0x7fffffffu);
         if (SUM) sum[k] += v[k];
       }
+    };
+    int64_t r = r0 + tr;
+    for (; r + 24 < r1; r += 32) {  // four rows' loads together
+      typename E::Raw raw[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[i] = load_row8<E>((const S*)a.x + (r + 8 * i) * a.ldx, c, a.cols);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add(raw[i]);
     }
+    for (; r < r1; r += 8) add(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols));
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
@@ -462,70 +476,84 @@ __global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
 }
 
 // A tile of 128 rows x 64 columns: a thread quantises 4 rows of 8 columns, and the tile
-// leaves through shared memory as 128 bytes of each of its columns.
+// leaves through shared memory as 128 bytes of each of its columns, 8 lanes a column.
 template <class E, bool SUM>
 __global__ __launch_bounds__(256) void col_quant_kernel(QuantArgs a) {
   using S = typename E::S;
-  constexpr int LD = 132;  // bytes of a column in shared memory: 33 banks
-  __shared__ uint32_t tile[64 * LD / 4];
+  constexpr int LD = 33;  // words of a column in shared memory: rows and columns on distinct banks
+  __shared__ uint32_t tile[64 * LD];
   __shared__ uint32_t pm[4][64];
   __shared__ float ps[SUM ? 4 : 1][64];
-  __shared__ float tops[64];
+  using E8 = Eight<float, sizeof(S) == 2>;
+  __shared__ E8 eights[64];
   const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
   const bool first = blockIdx.y == 0;
-  {
-    const int tc = threadIdx.x & 63, tr = threadIdx.x >> 6;
-    uint32_t m = 0;
-    float s = 0.f;
-    if (c0 + tc < a.cols) {
-      for (int i = tr; i < a.nrb; i += 4) {
-        m = max(m, *gptr(a.part_max + (int64_t)i * a.cols + c0 + tc));
-        if (SUM && first) s += *gptr(a.part_sum + (int64_t)i * a.cols + c0 + tc);
-      }
-    }
-    pm[tr][tc] = m;
-    if (SUM) ps[tr][tc] = s;
-    __syncthreads();
-    if (tr == 0) {
-      m = max(max(pm[0][tc], pm[1][tc]), max(pm[2][tc], pm[3][tc]));
-      tops[tc] = __uint_as_float(m);
-      if (first && c0 + tc < a.cols) {
-        a.scale[c0 + tc] = Eight<float>(__uint_as_float(m)).scale(1.f);
-        if (SUM) E::store1((S*)a.sum + c0 + tc, (ps[0][tc] + ps[1][tc]) + (ps[2][tc] + ps[3][tc]));
-      }
-    }
-    __syncthreads();
-  }
   const int tc = threadIdx.x & 7, tr = threadIdx.x >> 3;
   const int64_t c = c0 + 8 * tc;
-  float v[4][8];
+  // the tile is on its way while the columns' statistics are joined
+  typename E::Raw raw[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t r = r0 + 4 * tr + i;
-    if (r < a.rows && c < a.cols) {
-      E::expand(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols), v[i]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
-    }
+    raw[i] = r < a.rows && c < a.cols ? load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols) : typename E::Raw{};
   }
+  {
+    const int jc = threadIdx.x & 63, jr = threadIdx.x >> 6;
+    uint32_t m = 0;
+    float s = 0.f;
+    if (c0 + jc < a.cols) {
+#pragma unroll 4
+      for (int i = jr; i < a.nrb; i += 4) {
+        m = max(m, *gptr(a.part_max + (int64_t)i * a.cols + c0 + jc));
+        if (SUM && first) s += *gptr(a.part_sum + (int64_t)i * a.cols + c0 + jc);
+      }
+    }
+    pm[jr][jc] = m;
+    if (SUM) ps[jr][jc] = s;
+    __syncthreads();
+    if (jr == 0) {
+      m = max(max(pm[0][jc], pm[1][jc]), max(pm[2][jc], pm[3][jc]));
+      const E8 e(__uint_as_float(m));
+      eights[jc] = e;
+      if (first && c0 + jc < a.cols) {
+        a.scale[c0 + jc] = e.scale(1.f);
+        if (SUM) E::store1((S*)a.sum + c0 + jc, (ps[0][jc] + ps[1][jc]) + (ps[2][jc] + ps[3][jc]));
+      }
+    }
+    __syncthreads();
+  }
+  float v[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) E::expand(raw[i], v[i]);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const Eight<float> e(tops[8 * tc + k]);
-    uint32_t q = 0;
+    const E8 e = eights[8 * tc + k];
+    uint32_t n[4];
+    float rest = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q |= ((uint32_t)e(v[i][k]) & 0xffu) << (8 * i);
-    tile[(8 * tc + k) * (LD / 4) + tr] = q;
+    for (int i = 0; i < 4; ++i) n[i] = e.fast(v[i][k], rest);
+    if (!e.sure(rest)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n[i] = (uint32_t)e.exactly(v[i][k]);
+    }
+    tile[(8 * tc + k) * LD + tr] = low_bytes(n[0], n[1], n[2], n[3]);
   }
   __syncthreads();
-  const int col = threadIdx.x >> 2, piece = threadIdx.x & 3;  // 32 bytes of a column each
-  if (c0 + col >= a.cols) return;
-  int8_t* out = a.q + (c0 + col) * a.ldq;
-  const uint32_t* src = tile + col * (LD / 4) + 8 * piece;
+  const int piece = threadIdx.x & 7;  // 16 bytes of a column each
+  const int64_t r = r0 + 16 * piece;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int64_t r = r0 + 32 * piece + 8 * k;
-    if (r < a.rows) store_q8(out, r, a.rows, u32x2b_t{src[2 * k], src[2 * k + 1]});
+  for (int i = 0; i < 2; ++i) {
+    const int col = 32 * i + (threadIdx.x >> 3);
+    if (c0 + col >= a.cols || r >= a.rows) continue;
+    int8_t* out = a.q + (c0 + col) * a.ldq;
+    const uint32_t* src = tile + col * LD + 4 * piece;
+    const u32x4b_t w = {src[0], src[1], src[2], src[3]};
+    if (r + 16 <= a.rows) {
+      *(PRM_GLOBAL u32x4b_t*)(out + r) = w;
+    } else {
+      store_q8(out, r, a.rows, u32x2b_t{w[0], w[1]});
+      if (r + 8 < a.rows) store_q8(out, r + 8, a.rows, u32x2b_t{w[2], w[3]});
+    }
   }
 }
 
