@@ -209,7 +209,7 @@ int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres
 
 uint64_t prm_rms_norm_backward_workspace(int64_t rows, int64_t cols) {
   if (rows < 1 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return 0;
-  return (uint64_t)rms_norm_grad_parts(rows, cols) * (uint64_t)cols * 4;
+  return (uint64_t)rms_norm_grad_parts(OP_BF16, rows, cols) * (uint64_t)cols * 4;
 }
 
 int prm_rms_norm_backward(const void* gy, int64_t ldgy, const void* gh, int64_t ldgh, const void* h, int64_t ldh,
@@ -233,7 +233,7 @@ int prm_rms_norm_backward(const void* gy, int64_t ldgy, const void* gh, int64_t 
                              optional(dw, "dw", es), optional(dw ? workspace : nullptr, "workspace", 16)}));
   }
   NormGradArgs a = {gy, gh, h, w, dx, dw, (float*)workspace, rows, cols, ldgy, ldgh, ldh, lddx, eps,
-                    rms_norm_grad_parts(rows, cols)};
+                    rms_norm_grad_parts((OpType)dtype, rows, cols)};
   return launched(call, launch_rms_norm_grad((OpType)dtype, a, (hipStream_t)hip_stream));
 }
 

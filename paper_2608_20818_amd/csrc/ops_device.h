@@ -118,54 +118,72 @@ __device__ __forceinline__ void store_q8(int8_t* row, int64_t c, int64_t cols, c
 
 // ---- 8 bits ----------------------------------------------------------------------
 // q = the whole number nearest to 127 u / top, ties to even, decided exactly.  In fp32,
-// adding 1.5 * 2^23 to u inv (inv = 127 / top) rounds it to a whole number, which the
-// sum's low byte holds; what is left over says how far from the border of two whole
-// numbers it fell.  inv is off by 2 * 2^-24 at most, and u by 2^-24 (fp32 products: none):
-// 127 * 3 * 2^-24 = 2.3e-5, so where the remainder stays 3e-5 clear of 1/2 the number is
-// right.  Otherwise (in 1 of 2000 groups of 8) fp64 decides by comparing 254 |u| with
-// (2 k + 1) top, which it holds exactly (products of fp32 values: to its last bit).  Rows
-// too small or too large for fp32 are left to fp64 as a whole.  Five instructions a
-// value; checking each value apart took twelve, and bound the quantisers.
-template <typename U, bool EXACT32>
+// adding 1.5 * 2^23 to u inv (inv = 127 / top) rounds the product, unrounded before, to a
+// whole number, which the sum's low byte holds.  inv alone is inexact, and where that
+// could move a value over a border of two whole numbers depends on what u is:
+//
+// VALUES: u and top are values of a 16-bit type, U 2^a and T 2^b with whole U, T < 2^11.
+// The quotient is 127 U / (T 2^j), and off a border k + 1/2 by a whole multiple of
+// 1 / (2 T 2^j), which is (k + 1/2) / 254 U or more: at least 1.9e-6 of the border.  With inv
+// rounded UP (an error of less than 2^-23 = 1.2e-7) only values ON a border can fall
+// wrong.  There 127 U = T 2^(j-1) (2 k + 1), so the prime 127 divides 2 k + 1, which is
+// k = 63 alone, where the upwards error gives the even 64; or it divides T, one number
+// for the whole row, whose values are then decided by themselves.
+//
+// PRODUCT32, WIDE: u is a product of bf16 values (16 bits), or any fp32 or fp64 value.  What
+// the rounding leaves over says how far from the border it fell.  inv is off by 3 * 2^-24 at
+// most, and u by 2^-24 (fp32 products: none): 127 * 4 * 2^-24 = 3.1e-5, so where the
+// remainder stays 4e-5 clear of 1/2 the number is right.
+//
+// Otherwise, and in rows too small or too large for fp32, comparing 254 |u| with
+// (2 k + 1) top decides, in a type that holds both exactly: fp32 (24 bits) but for WIDE,
+// which takes fp64 (products of fp32 values: to its last bit).
+// 16384 x 4096 bf16 rows: 34 us; with a check for each value 38, for each 8 values 45
+// (values on a border, half the largest above all, are common there).
+enum EightKind { VALUES, PRODUCT32, WIDE };
+template <typename U, EightKind K>
 struct Eight {
-  using X = std::conditional_t<EXACT32, float, double>;
+  using X = std::conditional_t<K == WIDE, double, float>;
   U top;      // max |u| of the row
   float inv;  // 0: every q is 0 (a row of zeros, or one with a value that is not finite)
-  bool fp32;  // fp32 decides where it can
+  bool fp32;  // fp32 decides: always (VALUES), or where it can
   __device__ __forceinline__ Eight() {}
   __device__ __forceinline__ explicit Eight(U t) : top(t) {
     fp32 = t > (U)1e-35f && t < (U)3e38f;
     inv = fp32 ? 127.f / (float)t : 0.f;
+    if (fmaf(inv, (float)t, -127.f) < 0.f && fp32) inv = __uint_as_float(__float_as_uint(inv) + 1);
+    if constexpr (K == VALUES) fp32 = fp32 && ((__float_as_uint(t) & 0x7fffffu) | 0x800000u) % 127u != 0;
   }
   __device__ __forceinline__ bool finite() const { return top < (U)__builtin_huge_valf(); }
-  __device__ __forceinline__ int whole(U u, int k) const {  // k or k + 1 of |u|
-    return side((X)254 * (X)(u < 0 ? -u : u), (X)(2 * k + 1) * (X)top, u, k);
-  }
+  // k or k + 1 of |u|
   template <typename Y>
-  __device__ __forceinline__ static int side(Y l, Y r, U u, int k) {
+  __device__ __forceinline__ int side(U u, int k) const {
+    const Y l = (Y)254 * (Y)(u < 0 ? -u : u), r = (Y)(2 * k + 1) * (Y)top;
     const int q = l > r ? k + 1 : l < r ? k : k + (k & 1);
     return u < 0 ? -q : q;
   }
-  // the floor of the quotient; next to a whole number it may be the one below: the same q
+  // From the floor of the quotient; next to a whole number that may be the one below, with
+  // the same q.
   __device__ __forceinline__ int exactly(U u) const {
-    if (fp32) return whole(u, (int)floorf(fabsf((float)u * inv)));
+    if (inv > 0.f) return side<X>(u, (int)floorf(fabsf((float)u * inv)));
     if (!(top > (U)0) || !finite()) return 0;
-    const int k = (int)floor(127.0 * (fabs((double)u) / (double)top));
-    return side(254.0 * fabs((double)u), (2 * k + 1) * (double)top, u, k);
+    return side<double>(u, (int)floor(127.0 * (fabs((double)u) / (double)top)));
   }
   // q of one value in the low byte; `rest`: the largest |remainder| so far
   __device__ __forceinline__ uint32_t fast(U u, float& rest) const {
     constexpr float kMagic = 12582912.f;
     const float n = fmaf((float)u, inv, kMagic);
-    rest = fmaxf(rest, fabsf(fmaf((float)u, inv, kMagic - n)));
+    if constexpr (K != VALUES) rest = fmaxf(rest, fabsf(fmaf((float)u, inv, kMagic - n)));
     return __float_as_uint(n);
   }
-  __device__ __forceinline__ bool sure(float rest) const { return fp32 && rest < 0.49997f; }
+  __device__ __forceinline__ bool sure(float rest) const { return K == VALUES ? fp32 : fp32 && rest < 0.49996f; }
   // the scale: factor * top / 127; a row with a value that is not finite has NaN
   __device__ __forceinline__ float scale(float factor) const {
     return finite() ? (float)((double)factor * (double)top / 127.0) : __builtin_nanf("");
   }
 };
+// the rounding of a type's own values
+template <class E> using EightOf = Eight<float, std::is_same_v<typename E::S, float> ? WIDE : VALUES>;
 // the low bytes of four words
 __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);

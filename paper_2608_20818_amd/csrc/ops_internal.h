@@ -58,7 +58,7 @@ struct NormGradArgs {
   int32_t nparts;
 };
 hipError_t launch_rms_norm_grad(OpType t, const NormGradArgs& a, hipStream_t s);
-int32_t rms_norm_grad_parts(int64_t rows, int64_t cols);
+int32_t rms_norm_grad_parts(OpType t, int64_t rows, int64_t cols);  // most for 16-bit types
 
 // ---- products (ops_matmul.hip) -------------------------------------------------
 struct ProductArgs {

@@ -64,8 +64,8 @@ __device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_sum
   }
 }
 
-template <class U, bool X>
-__device__ __forceinline__ u32x2b_t eight8(const Eight<U, X>& e, const U u[8]) {
+template <class U, EightKind K>
+__device__ __forceinline__ u32x2b_t eight8(const Eight<U, K>& e, const U u[8]) {
   uint32_t n[8];
   float rest = 0.f;
 #pragma unroll
@@ -160,7 +160,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a)
   if constexpr (MODE == QUANT) top.m = raw_top.bits();
   row_reduce<TPR, U>(ss, top, MODE != QUANT, MODE != NORM, rs, rt);
   const float r = MODE == QUANT ? 1.f : 1.f / sqrtf(ss / (float)cols + a.eps);
-  const Eight<U, sizeof(S) == 2 && (MODE == QUANT || std::is_same_v<E, TBF16>)> eight(top.value());
+  using R = std::conditional_t<MODE == QUANT, EightOf<E>, Eight<U, std::is_same_v<E, TBF16> ? PRODUCT32 : WIDE>>;
+  const R eight(top.value());
   if (MODE != NORM && t == 0) a.scale[row] = eight.scale(r);
   auto out = [&](int64_t c, const typename E::Raw& raw) __attribute__((always_inline)) {
     float v[8], f[8];
@@ -240,18 +241,21 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // gradient
 // ---------------------------------------------------------------------------
-// A row's threads keep their columns' share of dw over all the rows that they take
-// (row, row + step, ...), and leave it as one row of `part`; a second kernel adds those
-// rows in order.  NCH 0 (rows over 32768): two sweeps a row, and dw in `part` itself.
+// A row's threads (TPR; 64: four rows a block of 256) keep their columns' share of dw over
+// all the rows that they take (row, row + step, ...), and a block leaves it as one row of
+// `part`; a second kernel adds those rows in order.  The next row is on its way while one
+// is summed.  NCH 0 (rows over 32768): two sweeps a row, and dw in `part` itself.
 template <class E, int TPR, int NCH>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGradArgs a) {
   using S = typename E::S;
-  constexpr int WPB = TPR == 64 ? 1 : TPR / 64;
+  constexpr int WPB = TPR == 64 ? 4 : TPR / 64;
   __shared__ float red[2][2][WPB];
+  __shared__ float share[TPR == 64 ? 4 : 1][TPR == 64 ? 512 : 1];
+  static_assert(TPR > 64 || NCH == 1, "the share of a wave");
   const int t = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
-  const int part = TPR == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (part >= a.nparts) return;  // whole waves, and no barrier below (TPR 64)
+  const int wave = threadIdx.x >> 6;
   const int64_t cols = a.cols;
+  const int64_t step = (int64_t)gridDim.x * (TPR == 64 ? 4 : 1);
   const S* w = (const S*)a.w;
   constexpr int N = NCH ? NCH : 1;
   float dw[N][8];
@@ -266,15 +270,30 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
       for (int k = 0; k < 8; ++k) v[k] = 1.f;
     }
   };
-  float* const mine = a.part + (int64_t)part * cols;
+  float* const mine = a.part + (int64_t)blockIdx.x * cols;
   bool first = true;
   int flip = 0;
-  for (int64_t row = part; row < a.rows; row += a.nparts) {
+  // the registers of a block of 1024 hold no second row of two pieces of fp32, or of four
+  constexpr bool AHEAD = NCH > 0 && (TPR < 1024 || NCH * sizeof(S) <= 4);
+  typename E::Raw rh[N], rg[N], rs[N];
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * TPR + t);
+      if (c < cols) {
+        rh[i] = load_row8<E>((const S*)a.h + row * a.ldh, c, cols);
+        rg[i] = load_row8<E>((const S*)a.gy + row * a.ldgy, c, cols);
+        if (a.gh) rs[i] = load_row8<E>((const S*)a.gh + row * a.ldgh, c, cols);
+      }
+    }
+  };
+  int64_t row = TPR == 64 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  if (AHEAD && row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
     const S* gy = (const S*)a.gy + row * a.ldgy;
     const S* h = (const S*)a.h + row * a.ldh;
     const S* gh = a.gh ? (const S*)a.gh + row * a.ldgh : nullptr;
     S* dx = (S*)a.dx + row * a.lddx;
-    typename E::Raw rh[N], rg[N];
     float ss = 0.f, sg = 0.f;  // sums of h^2 and of g h
     auto stats = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg) __attribute__((always_inline)) {
       float v[8], g[8], f[8];
@@ -287,19 +306,20 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
         sg += g[k] * f[k] * v[k];
       }
     };
+    typename E::Raw ch[N], cg[N], cs[N];
     if constexpr (NCH) {
+      if (!AHEAD) fetch(row);
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int64_t c = 8 * ((int64_t)i * TPR + t);
-        if (c < cols) {
-          rh[i] = load_row8<E>(h, c, cols);
-          rg[i] = load_row8<E>(gy, c, cols);
-        }
+        ch[i] = rh[i];
+        cg[i] = rg[i];
+        if (a.gh) cs[i] = rs[i];
       }
+      if (AHEAD && row + step < a.rows) fetch(row + step);
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int64_t c = 8 * ((int64_t)i * TPR + t);
-        if (c < cols) stats(c, rh[i], rg[i]);
+        if (c < cols) stats(c, ch[i], cg[i]);
       }
     } else {
       for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, load_row8<E>(h, c, cols), load_row8<E>(gy, c, cols));
@@ -309,8 +329,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
     if constexpr (TPR > 64) {
       // two sets of slots in turn: a wave writes the next row's behind one barrier only
       if ((threadIdx.x & 63) == 0) {
-        red[flip][0][threadIdx.x >> 6] = ss;
-        red[flip][1][threadIdx.x >> 6] = sg;
+        red[flip][0][wave] = ss;
+        red[flip][1][wave] = sg;
       }
       __syncthreads();
       ss = sg = 0.f;
@@ -323,7 +343,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
     }
     const float r = 1.f / sqrtf(ss / (float)cols + a.eps);
     const float coef = r * r * (sg / (float)cols);  // mean(g n) r: what each h is scaled by
-    auto out = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, float d[8]) __attribute__((always_inline)) {
+    auto out = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, const typename E::Raw& xs, float d[8]) __attribute__((always_inline)) {
       float v[8], g[8], f[8], o[8];
       E::expand(xh, v);
       E::expand(xg, g);
@@ -333,8 +353,8 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
         d[k] += g[k] * (v[k] * r);
         o[k] = r * (g[k] * f[k] - v[k] * coef);
       }
-      if (gh) {
-        E::expand(load_row8<E>(gh, c, cols), v);
+      if (a.gh) {
+        E::expand(xs, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] += v[k];
       }
@@ -344,14 +364,15 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int64_t c = 8 * ((int64_t)i * TPR + t);
-        if (c < cols) out(c, rh[i], rg[i], dw[i]);
+        if (c < cols) out(c, ch[i], cg[i], cs[i], dw[i]);
       }
     } else {
       for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
         float d[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) d[k] = first || c + k >= cols || !a.dw ? 0.f : mine[c + k];
-        out(c, load_row8<E>(h, c, cols), load_row8<E>(gy, c, cols), d);
+        const typename E::Raw xh = load_row8<E>(h, c, cols);
+        out(c, xh, load_row8<E>(gy, c, cols), gh ? load_row8<E>(gh, c, cols) : xh, d);
         if (a.dw)
           for (int k = 0; k < 8 && c + k < cols; ++k) mine[c + k] = d[k];
       }
@@ -359,7 +380,13 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
     }
   }
   if (!a.dw) return;
-  if constexpr (NCH) {
+  if constexpr (TPR == 64) {
+    // the block's four waves, added in order
+#pragma unroll
+    for (int k = 0; k < 8; ++k) share[wave][8 * t + k] = dw[0][k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += 256) mine[c] = (share[0][c] + share[1][c]) + (share[2][c] + share[3][c]);
+  } else if constexpr (NCH) {
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int64_t c = 8 * ((int64_t)i * TPR + t);
@@ -375,24 +402,24 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
   }
 }
 
-// dw[c] = sum over parts, in order: 8 threads a column take each eighth part, and
-// their sums are added in order.
+// dw[c] = sum over parts, in order: 32 threads a column take each 32nd part, and their
+// sums are added in order.
 template <class E>
-__global__ __launch_bounds__(256) void part_sum_kernel(const float* part, int nparts, int64_t cols, typename E::S* out) {
-  __shared__ float red[8][32];
+__global__ __launch_bounds__(1024) void part_sum_kernel(const float* part, int nparts, int64_t cols, typename E::S* out) {
+  __shared__ float red[32][33];
   const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + tc;
   float s = 0.f;
   if (c < cols) {
 #pragma unroll 8
-    for (int i = tr; i < nparts; i += 8) s += *gptr(part + (int64_t)i * cols + c);
+    for (int i = tr; i < nparts; i += 32) s += *gptr(part + (int64_t)i * cols + c);
   }
   red[tr][tc] = s;
   __syncthreads();
   if (tr == 0 && c < cols) {
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += red[i][tc];
+    for (int i = 0; i < 32; ++i) s += red[i][tc];
     E::store1(out + c, s);
   }
 }
@@ -401,8 +428,8 @@ template <class E>
 hipError_t launch_grad(const NormGradArgs& a, hipStream_t s) {
   const int64_t pieces = (a.cols + 7) / 8;
   if (a.rows > 0) {
-    const dim3 waves((unsigned)((a.nparts + 3) / 4)), blocks((unsigned)a.nparts);
-#define PRM_GRAD(TPR, NCH) norm_grad_kernel<E, TPR, NCH><<<TPR == 64 ? waves : blocks, TPR == 64 ? 256 : TPR, 0, s>>>(a)
+    const unsigned blocks = (unsigned)a.nparts;
+#define PRM_GRAD(TPR, NCH) norm_grad_kernel<E, TPR, NCH><<<blocks, TPR == 64 ? 256 : TPR, 0, s>>>(a)
     if (pieces <= 64) PRM_GRAD(64, 1);
     else if (pieces <= 256) PRM_GRAD(256, 1);
     else if (pieces <= 512) PRM_GRAD(256, 2);
@@ -415,7 +442,7 @@ hipError_t launch_grad(const NormGradArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (a.dw)
-    part_sum_kernel<E><<<(unsigned)((a.cols + 31) / 32), 256, 0, s>>>(a.part, a.rows > 0 ? a.nparts : 0, a.cols, (typename E::S*)a.dw);
+    part_sum_kernel<E><<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a.part, a.rows > 0 ? a.nparts : 0, a.cols, (typename E::S*)a.dw);
   return hipGetLastError();
 }
 
@@ -484,7 +511,7 @@ __global__ __launch_bounds__(256) void col_quant_kernel(QuantArgs a) {
   __shared__ uint32_t tile[64 * LD];
   __shared__ uint32_t pm[4][64];
   __shared__ float ps[SUM ? 4 : 1][64];
-  using E8 = Eight<float, sizeof(S) == 2>;
+  using E8 = EightOf<E>;
   __shared__ E8 eights[64];
   const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
   const bool first = blockIdx.y == 0;
@@ -605,11 +632,13 @@ hipError_t launch_quantize_cols(OpType t, const QuantArgs& a, hipStream_t s) {
   return t == OP_F32 ? launch_cols<TF32>(a, s) : t == OP_BF16 ? launch_cols<TBF16>(a, s) : launch_cols<TF16>(a, s);
 }
 
-// Rows of partial dw: one a block (a wave, for short rows), enough to fill the card and
-// few against the rows.
-int32_t rms_norm_grad_parts(int64_t rows, int64_t cols) {
-  const int64_t most = cols <= 512 ? 2048 : cols <= 4096 ? 1024 : 512;
-  return (int32_t)(rows < most ? (rows < 1 ? 1 : rows) : most);
+// Blocks, each of which leaves a row of partial dw: as many as the card holds at once (of
+// 256 threads four a CU, two with two pieces of fp32; of 1024 one), so that none waits for
+// another to end.  A block of short rows takes four at a time.  8192 x 4096 bf16: 55 us
+// with 1024, 62 with 512; fp32 117 and 105; 2048 x 16384 bf16 59 us with 256, 68 with 512.
+int32_t rms_norm_grad_parts(OpType t, int64_t rows, int64_t cols) {
+  const int64_t most = cols > 4096 ? 256 : cols > 2048 && t == OP_F32 ? 512 : 1024, groups = cols <= 512 ? (rows + 3) / 4 : rows;
+  return (int32_t)(groups < most ? (groups < 1 ? 1 : groups) : most);
 }
 
 hipError_t launch_rms_norm_grad(OpType t, const NormGradArgs& a, hipStream_t s) {
