@@ -347,7 +347,7 @@ int prm_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
 /* x in 8 bits with a scale for each COLUMN, transposed: q (cols x rows, leading
  * dimension ldq >= rows), scale (cols), and, unless `sum` is NULL, the columns'
  * sums over the rows (cols values of type dtype, added in fp32 in a fixed order; the
- * gradient of a bias).  1 <= rows <= 2^22, cols <= 2^24.  `workspace`:
+ * gradient of a bias).  1 <= rows <= 2^22, cols <= 2^24, less than 2^24 tiles of 128 x 64.  `workspace`:
  * prm_quantize_cols_workspace(rows, cols) bytes, 16-byte aligned, used by this
  * call only. */
 uint64_t prm_quantize_cols_workspace(int64_t rows, int64_t cols);
@@ -369,6 +369,27 @@ int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const in
                     const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo,
                     int64_t m, int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes,
                     void* hip_stream);
+
+/* A linear layer with its products in 8 bits: y = Q(x) Q(w)^T + bias, for x (m x k), w
+ * (n x k), bias (n values, or NULL) and y (m x n), all of type dtype; Q quantises each
+ * row as prm_quantize_rows does.  m, n, k <= 131071.  What prm_quantize_rows of x and
+ * of w and prm_int8_matmul give, bit for bit, in fewer launches.  `workspace`:
+ * prm_int8_linear_workspace(m, n, k) bytes, 16-byte aligned, used by this call only. */
+uint64_t prm_int8_linear_workspace(int64_t m, int64_t n, int64_t k);
+int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, int32_t dtype, void* y,
+                    int64_t ldy, int64_t m, int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes,
+                    void* hip_stream);
+
+/* Its gradients from gy (m x n), those of the unquantised layer with their products in
+ * 8 bits, each operand quantised along the sum that it enters:
+ *   dx = Q(gy) Q(w^T)^T   (m x k)      dw = Q(gy^T) Q(x^T)^T   (n x k)
+ *   db = the columns' sums of gy       (n values; fp32 in a fixed order)
+ * of type dtype; each may be NULL (x is then not read for dw, w not for dx).  m >= 1.
+ * `workspace`: prm_int8_linear_backward_workspace(m, n, k) bytes, as above. */
+uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k);
+int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                             int32_t dtype, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, int64_t m,
+                             int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes, void* hip_stream);
 
 /* Root-mean-square norm of each row of x (rows x cols), after the residual's
  * addition where `residual` is not NULL:

@@ -134,7 +134,11 @@ def load() -> ctypes.CDLL:
     L.prm_rms_norm_backward_workspace.argtypes = [i64, i64]
     L.prm_rms_norm_backward_workspace.restype = u64
     L.prm_rms_norm_backward.argtypes = [P, i64, P, i64, P, i64, P, i32, i64, i64, f32, P, i64, P, P, u64, P]
-    for name in ("prm_quantize_rows", "prm_quantize_cols", "prm_int8_matmul", "prm_rms_norm", "prm_rms_norm_backward"):
+    L.prm_int8_linear_workspace.argtypes = L.prm_int8_linear_backward_workspace.argtypes = [i64, i64, i64]
+    L.prm_int8_linear_workspace.restype = L.prm_int8_linear_backward_workspace.restype = u64
+    L.prm_int8_linear.argtypes = [P, i64, P, i64, P, i32, P, i64, i64, i64, i64, P, u64, P]
+    L.prm_int8_linear_backward.argtypes = [P, i64, P, i64, P, i64, i32, P, i64, P, i64, P, i64, i64, i64, P, u64, P]
+    for name in ("prm_int8_linear", "prm_int8_linear_backward", "prm_quantize_rows", "prm_quantize_cols", "prm_int8_matmul", "prm_rms_norm", "prm_rms_norm_backward"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

@@ -2,10 +2,11 @@
 // outputs' allocation and the call into libprm, natively.  In Python they cost 15 to 25 us a
 // call, several times the GPU's for one token.
 //
-// Every function returns what the operator does, a negative PRM_E* code that libprm gave
-// (the caller raises it), or None: not a plain call (a tensor subclass, another device
-// than the current one, a layout that needs a copy, a type or shape that is wrong, a
-// gradient to record), and the Python binding then takes or refuses it.
+// Every function returns what the operator does (with the gradients' node, where one is
+// to be recorded), a negative PRM_E* code that libprm gave (the caller raises it), or None:
+// not a plain call (a tensor subclass, another device than the current one, a layout
+// that needs a copy, a type or shape that is wrong), and the Python binding then takes or
+// refuses it.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
@@ -13,6 +14,8 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -89,57 +92,33 @@ bool optional(PyObject* o, const at::Tensor** t) {
 }
 const void* data(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
 
+// A call that libprm refused.
+struct Refused : std::runtime_error {
+  int code;
+  explicit Refused(int rc) : std::runtime_error("libprm error " + std::to_string(rc) + ": " + prm_last_error()), code(rc) {}
+};
+void check(int rc) {
+  if (rc < 0) throw Refused(rc);
+}
 template <class F>
 PyObject* guarded(F&& f) {
   try {
     return f();
+  } catch (const Refused& e) {
+    return PyLong_FromLong(e.code);
   } catch (const std::exception& e) {  // out of memory above all
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;
   }
 }
 
-// ---- the operators on checked tensors; a negative code where libprm refuses ------------
-struct Eight {
-  at::Tensor q, scale, sum;
-  Rows r;  // of q
-  int rc = 0;
-};
-Eight rows_in_eight(const at::Tensor& x, const Rows& r) {
-  Eight e;
-  const c10::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
-  e.q = eight_bits(lead, r.cols, x, &e.r.ld);
-  e.r.rows = r.rows;
-  e.r.cols = r.cols;
-  e.scale = empty(lead, at::kFloat, x);
-  e.rc = prm_quantize_rows(x.const_data_ptr(), code_of(x.scalar_type()), r.rows, r.cols, r.ld, (int8_t*)e.q.data_ptr(), e.r.ld,
-                           (float*)e.scale.data_ptr(), stream());
-  return e;
-}
-Eight cols_in_eight(const at::Tensor& x, const Rows& r, bool with_sum) {
-  Eight e;
-  e.q = eight_bits({r.cols}, r.rows, x, &e.r.ld);
-  e.r.rows = r.cols;
-  e.r.cols = r.rows;
-  e.scale = empty({r.cols}, at::kFloat, x);
-  if (with_sum) e.sum = empty({r.cols}, x.scalar_type(), x);
-  const uint64_t need = prm_quantize_cols_workspace(r.rows, r.cols);
-  at::Tensor ws = empty({(int64_t)need}, at::kByte, x);
-  e.rc = prm_quantize_cols(x.const_data_ptr(), code_of(x.scalar_type()), r.rows, r.cols, r.ld, (int8_t*)e.q.data_ptr(), e.r.ld,
-                           (float*)e.scale.data_ptr(), with_sum ? e.sum.data_ptr() : nullptr, ws.data_ptr(), need, stream());
-  return e;
-}
-int product(const at::Tensor& a, const Rows& ra, const at::Tensor& sa, const at::Tensor& b, const Rows& rb, const at::Tensor& sb,
-            const at::Tensor* bias, c10::IntArrayRef lead, int code, at::Tensor* out) {
+at::Tensor bytes(uint64_t n, const at::Tensor& like) { return n ? empty({(int64_t)n}, at::kByte, like) : at::Tensor(); }
+void* at_of(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+c10::IntArrayRef lead_of(const at::Tensor& t) { return t.sizes().slice(0, t.dim() - 1); }
+at::Tensor with_last(c10::IntArrayRef lead, int64_t n, const at::Tensor& like, at::ScalarType type) {
   c10::SmallVector<int64_t, 6> size(lead.begin(), lead.end());
-  size.push_back(rb.rows);
-  *out = empty(size, type_of(code), a);
-  const uint64_t need = prm_int8_matmul_workspace(ra.rows, rb.rows, ra.cols);
-  at::Tensor ws;
-  if (need) ws = empty({(int64_t)need}, at::kByte, a);
-  return prm_int8_matmul((const int8_t*)a.const_data_ptr(), ra.ld, (const float*)sa.const_data_ptr(), (const int8_t*)b.const_data_ptr(),
-                         rb.ld, (const float*)sb.const_data_ptr(), data(bias), code, out->data_ptr(), rb.rows, ra.rows, rb.rows, ra.cols,
-                         need ? ws.data_ptr() : nullptr, need, stream());
+  size.push_back(n);
+  return empty(size, type, like);
 }
 
 // quantize_rows(x)
@@ -149,22 +128,28 @@ PyObject* quantize_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor* x = plain(args[0]);
     Rows r;
     if (!x || code_of(x->scalar_type()) < 0 || !here(*x) || !rows_of(*x, &r)) Py_RETURN_NONE;
-    Eight e = rows_in_eight(*x, r);
-    if (e.rc < 0) return PyLong_FromLong(e.rc);
-    return Py_BuildValue("(NN)", wrap(std::move(e.q)), wrap(std::move(e.scale)));
+    int64_t ldq;
+    at::Tensor q = eight_bits(lead_of(*x), r.cols, *x, &ldq), s = empty(lead_of(*x), at::kFloat, *x);
+    check(prm_quantize_rows(x->const_data_ptr(), code_of(x->scalar_type()), r.rows, r.cols, r.ld, (int8_t*)q.data_ptr(), ldq,
+                            (float*)s.data_ptr(), stream()));
+    return Py_BuildValue("(NN)", wrap(std::move(q)), wrap(std::move(s)));
   });
 }
 
-// quantize_cols(x, with_sum)
+// quantize_cols(x)
 PyObject* quantize_cols(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 2) Py_RETURN_NONE;
+  if (n != 1) Py_RETURN_NONE;
   return guarded([&]() -> PyObject* {
     const at::Tensor* x = plain(args[0]);
     Rows r;
     if (!x || x->dim() != 2 || code_of(x->scalar_type()) < 0 || !here(*x) || !rows_of(*x, &r)) Py_RETURN_NONE;
-    Eight e = cols_in_eight(*x, r, args[1] == Py_True);
-    if (e.rc < 0) return PyLong_FromLong(e.rc);
-    return Py_BuildValue("(NNN)", wrap(std::move(e.q)), wrap(std::move(e.scale)), wrap(std::move(e.sum)));
+    int64_t ldq;
+    at::Tensor q = eight_bits({r.cols}, r.rows, *x, &ldq), s = empty({r.cols}, at::kFloat, *x);
+    const uint64_t need = prm_quantize_cols_workspace(r.rows, r.cols);
+    at::Tensor ws = bytes(need, *x);
+    check(prm_quantize_cols(x->const_data_ptr(), code_of(x->scalar_type()), r.rows, r.cols, r.ld, (int8_t*)q.data_ptr(), ldq,
+                            (float*)s.data_ptr(), nullptr, at_of(ws), need, stream()));
+    return Py_BuildValue("(NN)", wrap(std::move(q)), wrap(std::move(s)));
   });
 }
 
@@ -182,19 +167,88 @@ PyObject* int8_matmul(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a->scalar_type() != at::kChar || b->scalar_type() != at::kChar || !here(*a) || b->device() != a->device() || b->dim() != 2 ||
         !rows_of(*a, &ra) || !rows_of(*b, &rb) || ra.cols != rb.cols)
       Py_RETURN_NONE;
-    const c10::IntArrayRef lead = a->sizes().slice(0, a->dim() - 1);
-    if (sa->scalar_type() != at::kFloat || sa->sizes() != lead || !sa->is_contiguous() || sa->device() != a->device() ||
+    if (sa->scalar_type() != at::kFloat || sa->sizes() != lead_of(*a) || !sa->is_contiguous() || sa->device() != a->device() ||
         !vector_of(*sb, *a, at::kFloat, rb.rows) || (bias && !vector_of(*bias, *a, type_of(code), rb.rows)))
       Py_RETURN_NONE;
-    at::Tensor out;
-    const int rc = product(*a, ra, *sa, *b, rb, *sb, bias, lead, (int)code, &out);
-    if (rc < 0) return PyLong_FromLong(rc);
+    at::Tensor out = with_last(lead_of(*a), rb.rows, *a, type_of(code));
+    const uint64_t need = prm_int8_matmul_workspace(ra.rows, rb.rows, ra.cols);
+    at::Tensor ws = bytes(need, *a);
+    check(prm_int8_matmul((const int8_t*)a->const_data_ptr(), ra.ld, (const float*)sa->const_data_ptr(), (const int8_t*)b->const_data_ptr(),
+                          rb.ld, (const float*)sb->const_data_ptr(), data(bias), (int32_t)code, out.data_ptr(), rb.rows, ra.rows, rb.rows,
+                          ra.cols, at_of(ws), need, stream()));
     return wrap(std::move(out));
   });
 }
 
-// linear_forward(x, weight, bias): the layer's output
-PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+// ---- gradients -----------------------------------------------------------------------
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+// An absent argument: a Function takes no undefined tensor, and counts only those that are
+// there when it says whose gradients are needed.
+using Maybe = std::optional<at::Tensor>;
+Maybe maybe(const at::Tensor* t) { return t ? Maybe(*t) : Maybe(); }
+at::Tensor or_none(const Maybe& t) { return t ? *t : at::Tensor(); }
+
+// The gradients of gradients are refused, where they are asked for and not before.
+variable_list once(variable_list grads, bool recording) {
+  if (!recording) return grads;
+  for (at::Tensor& g : grads)
+    if (g.defined()) g = g.detach().set_requires_grad(true);
+  auto refuse = std::make_shared<torch::autograd::DelayedError>("these gradients are not differentiable", (int64_t)grads.size());
+  return (*refuse)(std::move(grads));
+}
+at::Tensor with_rows(const at::Tensor& t, Rows* r) {
+  if (rows_of(t, r)) return t;
+  at::Tensor c = t.contiguous();
+  rows_of(c, r);
+  return c;
+}
+
+at::Tensor linear(const at::Tensor& x, const at::Tensor& w, const at::Tensor& bias) {
+  Rows rx, rw;
+  rows_of(x, &rx);
+  rows_of(w, &rw);
+  at::Tensor y = with_last(lead_of(x), rw.rows, x, x.scalar_type());
+  const uint64_t need = prm_int8_linear_workspace(rx.rows, rw.rows, rx.cols);
+  at::Tensor ws = bytes(need, x);
+  check(prm_int8_linear(x.const_data_ptr(), rx.ld, w.const_data_ptr(), rw.ld, bias.defined() ? bias.const_data_ptr() : nullptr,
+                        code_of(x.scalar_type()), y.data_ptr(), rw.rows, rx.rows, rw.rows, rx.cols, at_of(ws), need, stream()));
+  return y;
+}
+
+struct Linear : torch::autograd::Function<Linear> {
+  static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, const Maybe& bias) {
+    ctx->save_for_backward({x, w});
+    ctx->saved_data["bias"] = bias.has_value();
+    return linear(x, w, or_none(bias));
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool recording = at::GradMode::is_enabled();
+    variable_list out(3);
+    {
+      at::AutoGradMode off(false);
+      const variable_list saved = ctx->get_saved_variables();
+      const at::Tensor &x = saved[0], &w = saved[1];
+      Rows rg, rx, rw;
+      const at::Tensor gy = with_rows(grads[0], &rg);
+      rows_of(x, &rx);
+      rows_of(w, &rw);
+      if (ctx->needs_input_grad(0)) out[0] = empty(x.sizes(), x.scalar_type(), x);
+      if (ctx->needs_input_grad(1)) out[1] = empty(w.sizes(), w.scalar_type(), w);
+      if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) out[2] = empty({rw.rows}, w.scalar_type(), w);
+      const uint64_t need = prm_int8_linear_backward_workspace(rx.rows, rw.rows, rx.cols);
+      at::Tensor ws = bytes(need, x);
+      check(prm_int8_linear_backward(gy.const_data_ptr(), rg.ld, x.const_data_ptr(), rx.ld, w.const_data_ptr(), rw.ld,
+                                     code_of(x.scalar_type()), at_of(out[0]), rx.cols, at_of(out[1]), rx.cols, at_of(out[2]), rx.rows,
+                                     rw.rows, rx.cols, at_of(ws), need, stream()));
+    }
+    return once(std::move(out), recording);
+  }
+};
+
+// int8_linear(x, weight, bias)
+PyObject* int8_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 3) Py_RETURN_NONE;
   return guarded([&]() -> PyObject* {
     const at::Tensor *x = plain(args[0]), *w = plain(args[1]), *bias;
@@ -203,123 +257,102 @@ PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
         w->scalar_type() != x->scalar_type() || w->device() != x->device() || !rows_of(*x, &rx) || !rows_of(*w, &rw) || rx.cols != rw.cols ||
         (bias && !vector_of(*bias, *x, x->scalar_type(), rw.rows)))
       Py_RETURN_NONE;
-    Eight ex = rows_in_eight(*x, rx);
-    if (ex.rc < 0) return PyLong_FromLong(ex.rc);
-    Eight ew = rows_in_eight(*w, rw);
-    if (ew.rc < 0) return PyLong_FromLong(ew.rc);
-    at::Tensor out;
-    const int rc = product(ex.q, ex.r, ex.scale, ew.q, ew.r, ew.scale, bias, x->sizes().slice(0, x->dim() - 1), code_of(x->scalar_type()), &out);
-    if (rc < 0) return PyLong_FromLong(rc);
-    return wrap(std::move(out));
+    const Maybe b = maybe(bias);
+    return wrap(records(x) || records(w) || records(bias) ? Linear::apply(*x, *w, b) : linear(*x, *w, or_none(b)));
   });
 }
 
-// linear_backward(gy, x, weight, need_x, need_w, need_b): (dx, dw, db)
-PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 6) Py_RETURN_NONE;
-  return guarded([&]() -> PyObject* {
-    const at::Tensor *gy = plain(args[0]), *x = plain(args[1]), *w = plain(args[2]);
-    Rows rg, rx, rw;
-    if (!gy || !x || !w || code_of(x->scalar_type()) < 0 || !here(*x) || gy->scalar_type() != x->scalar_type() || gy->device() != x->device() ||
-        w->scalar_type() != x->scalar_type() || w->device() != x->device() || !rows_of(*gy, &rg) || !rows_of(*x, &rx) || !rows_of(*w, &rw) ||
-        rg.rows != rx.rows || rg.cols != rw.rows || rx.cols != rw.cols)
-      Py_RETURN_NONE;
-    const bool need_x = args[3] == Py_True, need_w = args[4] == Py_True, need_b = args[5] == Py_True;
-    const int code = code_of(x->scalar_type());
-    at::Tensor dx, dw, db;
-    if (need_x) {
-      Eight g = rows_in_eight(*gy, rg);
-      if (g.rc < 0) return PyLong_FromLong(g.rc);
-      Eight ew = cols_in_eight(*w, rw, false);
-      if (ew.rc < 0) return PyLong_FromLong(ew.rc);
-      const int rc = product(g.q, g.r, g.scale, ew.q, ew.r, ew.scale, nullptr, x->sizes().slice(0, x->dim() - 1), code, &dx);
-      if (rc < 0) return PyLong_FromLong(rc);
-    }
-    if (need_w || need_b) {
-      Eight g = cols_in_eight(*gy, rg, need_b);
-      if (g.rc < 0) return PyLong_FromLong(g.rc);
-      db = g.sum;
-      if (need_w) {
-        Eight ex = cols_in_eight(*x, rx, false);
-        if (ex.rc < 0) return PyLong_FromLong(ex.rc);
-        const int64_t rows[1] = {rg.cols};
-        const int rc = product(g.q, g.r, g.scale, ex.q, ex.r, ex.scale, nullptr, rows, code, &dw);
-        if (rc < 0) return PyLong_FromLong(rc);
+// (y, h or nothing), or (q, scale, h or nothing)
+variable_list norm(const at::Tensor& x, const at::Tensor& w, const at::Tensor& res, float eps, bool quantize) {
+  Rows r, rr;
+  rows_of(x, &r);
+  if (res.defined()) rows_of(res, &rr);
+  at::Tensor h, y, q, s;
+  int64_t ldq = 0;
+  if (res.defined()) h = empty(x.sizes(), x.scalar_type(), x);
+  if (quantize) {
+    q = eight_bits(lead_of(x), r.cols, x, &ldq);
+    s = empty(lead_of(x), at::kFloat, x);
+  } else {
+    y = empty(x.sizes(), x.scalar_type(), x);
+  }
+  check(prm_rms_norm(x.const_data_ptr(), r.ld, res.defined() ? res.const_data_ptr() : nullptr, rr.ld,
+                     w.defined() ? w.const_data_ptr() : nullptr, code_of(x.scalar_type()), r.rows, r.cols, eps, at_of(h), r.cols, at_of(y),
+                     r.cols, (int8_t*)at_of(q), ldq, (float*)at_of(s), stream()));
+  variable_list out = quantize ? variable_list{q, s} : variable_list{y};
+  if (h.defined()) out.push_back(h);
+  return out;
+}
+
+struct Norm : torch::autograd::Function<Norm> {
+  static variable_list forward(AutogradContext* ctx, const at::Tensor& x, const Maybe& w, const Maybe& res, double eps) {
+    variable_list out = norm(x, or_none(w), or_none(res), (float)eps, false);
+    ctx->save_for_backward({res ? out[1] : x, or_none(w)});
+    ctx->saved_data["res"] = res.has_value();
+    ctx->saved_data["eps"] = eps;
+    ctx->set_materialize_grads(false);
+    return out;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool recording = at::GradMode::is_enabled();
+    variable_list out(4);
+    {
+      at::AutoGradMode off(false);
+      const variable_list saved = ctx->get_saved_variables();
+      const at::Tensor &h = saved[0], &w = saved[1];
+      const bool need_dw = w.defined() && ctx->needs_input_grad(1), kept = grads.size() > 1 && grads[1].defined();
+      at::Tensor dx;
+      if (!grads[0].defined()) {  // only the kept sum has a gradient
+        dx = kept ? grads[1] : at::Tensor();
+      } else {
+        Rows rg, rs, rh;
+        const at::Tensor gy = with_rows(grads[0], &rg), gh = kept ? with_rows(grads[1], &rs) : at::Tensor();
+        rows_of(h, &rh);
+        dx = empty(h.sizes(), h.scalar_type(), h);
+        at::Tensor ws;
+        uint64_t need = 0;
+        if (need_dw) {
+          out[1] = empty({rh.cols}, h.scalar_type(), h);
+          need = prm_rms_norm_backward_workspace(rh.rows, rh.cols);
+          ws = bytes(need, h);
+        }
+        check(prm_rms_norm_backward(gy.const_data_ptr(), rg.ld, kept ? gh.const_data_ptr() : nullptr, rs.ld, h.const_data_ptr(), rh.ld,
+                                    w.defined() ? w.const_data_ptr() : nullptr, code_of(h.scalar_type()), rh.rows, rh.cols,
+                                    (float)ctx->saved_data["eps"].toDouble(), dx.data_ptr(), rh.cols, at_of(out[1]), at_of(ws), need,
+                                    stream()));
       }
+      if (ctx->needs_input_grad(0)) out[0] = dx;
+      if (ctx->saved_data["res"].toBool() && ctx->needs_input_grad(w.defined() ? 2 : 1)) out[2] = dx;
     }
-    return Py_BuildValue("(NNN)", wrap(std::move(dx)), wrap(std::move(dw)), wrap(std::move(db)));
-  });
-}
+    return once(std::move(out), recording);
+  }
+};
 
-// rms_norm(x, weight, residual, eps, quantize, record): y, (y, h), (q, scale) or (q, scale, h);
-// None where a gradient is to be recorded, unless `record` says that the caller does that
+// rms_norm(x, weight, residual, eps, quantize): y, (y, h), (q, scale) or (q, scale, h)
 PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 6) Py_RETURN_NONE;
+  if (n != 5) Py_RETURN_NONE;
   return guarded([&]() -> PyObject* {
     const at::Tensor *x = plain(args[0]), *w, *res;
     if (!x || !optional(args[1], &w) || !optional(args[2], &res) || !PyFloat_CheckExact(args[3])) Py_RETURN_NONE;
-    const float eps = (float)PyFloat_AS_DOUBLE(args[3]);
-    const bool quantize = args[4] == Py_True;
-    if (args[5] != Py_True && (records(x) || records(w) || records(res))) Py_RETURN_NONE;
-    Rows r, rr;
-    const int code = code_of(x->scalar_type());
-    if (code < 0 || !here(*x) || !rows_of(*x, &r) || (w && !vector_of(*w, *x, x->scalar_type(), r.cols))) Py_RETURN_NONE;
-    if (res && (res->scalar_type() != x->scalar_type() || res->sizes() != x->sizes() || res->device() != x->device() || !rows_of(*res, &rr)))
+    const double eps = PyFloat_AS_DOUBLE(args[3]);
+    const bool quantize = args[4] == Py_True, record = records(x) || records(w) || records(res);
+    Rows r;
+    if ((quantize ? record : args[4] != Py_False) || code_of(x->scalar_type()) < 0 || !here(*x) || !rows_of(*x, &r) ||
+        (w && !vector_of(*w, *x, x->scalar_type(), r.cols)))
       Py_RETURN_NONE;
-    at::Tensor h, y, q, s;
-    int64_t ldq = 0;
-    if (res) h = empty(x->sizes(), x->scalar_type(), *x);
-    if (quantize) {
-      const c10::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
-      q = eight_bits(lead, r.cols, *x, &ldq);
-      s = empty(lead, at::kFloat, *x);
-    } else {
-      y = empty(x->sizes(), x->scalar_type(), *x);
-    }
-    const int rc = prm_rms_norm(x->const_data_ptr(), r.ld, data(res), rr.ld, data(w), code, r.rows, r.cols, eps, res ? h.data_ptr() : nullptr,
-                                r.cols, quantize ? nullptr : y.data_ptr(), r.cols, quantize ? (int8_t*)q.data_ptr() : nullptr, ldq,
-                                quantize ? (float*)s.data_ptr() : nullptr, stream());
-    if (rc < 0) return PyLong_FromLong(rc);
-    if (quantize)
-      return res ? Py_BuildValue("(NNN)", wrap(std::move(q)), wrap(std::move(s)), wrap(std::move(h)))
-                 : Py_BuildValue("(NN)", wrap(std::move(q)), wrap(std::move(s)));
-    return res ? Py_BuildValue("(NN)", wrap(std::move(y)), wrap(std::move(h))) : wrap(std::move(y));
-  });
-}
-
-// rms_norm_backward(gy, gh, h, weight, eps, need_dw): (dx, dw)
-PyObject* rms_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 6) Py_RETURN_NONE;
-  return guarded([&]() -> PyObject* {
-    const at::Tensor *gy = plain(args[0]), *gh, *h = plain(args[2]), *w;
-    if (!gy || !optional(args[1], &gh) || !h || !optional(args[3], &w) || !PyFloat_CheckExact(args[4])) Py_RETURN_NONE;
-    const bool need_dw = args[5] == Py_True;
-    Rows rg, rs, rh;
-    const int code = code_of(h->scalar_type());
-    if (code < 0 || !here(*h) || !rows_of(*h, &rh) || !rows_of(*gy, &rg) || (gh && !rows_of(*gh, &rs)) ||
-        (w && !vector_of(*w, *h, h->scalar_type(), rh.cols)))
+    if (res && (res->scalar_type() != x->scalar_type() || res->sizes() != x->sizes() || res->device() != x->device() || !rows_of(*res, &r)))
       Py_RETURN_NONE;
-    for (const at::Tensor* t : {gy, gh})
-      if (t && (t->scalar_type() != h->scalar_type() || t->sizes() != h->sizes() || t->device() != h->device())) Py_RETURN_NONE;
-    at::Tensor dx = empty(h->sizes(), h->scalar_type(), *h), dw, ws;
-    uint64_t need = 0;
-    if (need_dw) {
-      dw = empty({rh.cols}, h->scalar_type(), *h);
-      need = prm_rms_norm_backward_workspace(rh.rows, rh.cols);
-      ws = empty({(int64_t)need}, at::kByte, *h);
-    }
-    const int rc = prm_rms_norm_backward(gy->const_data_ptr(), rg.ld, data(gh), rs.ld, h->const_data_ptr(), rh.ld, data(w), code, rh.rows,
-                                         rh.cols, (float)PyFloat_AS_DOUBLE(args[4]), dx.data_ptr(), rh.cols, need_dw ? dw.data_ptr() : nullptr,
-                                         need_dw ? ws.data_ptr() : nullptr, need, stream());
-    if (rc < 0) return PyLong_FromLong(rc);
-    return Py_BuildValue("(NN)", wrap(std::move(dx)), wrap(std::move(dw)));
+    const Maybe wt = maybe(w), rt = maybe(res);
+    variable_list out = record ? Norm::apply(*x, wt, rt, eps) : norm(*x, or_none(wt), or_none(rt), (float)eps, quantize);
+    if (out.size() == 1) return wrap(std::move(out[0]));
+    if (out.size() == 2) return Py_BuildValue("(NN)", wrap(std::move(out[0])), wrap(std::move(out[1])));
+    return Py_BuildValue("(NNN)", wrap(std::move(out[0])), wrap(std::move(out[1])), wrap(std::move(out[2])));
   });
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef kMethods[] = {METHOD(quantize_rows), METHOD(quantize_cols),     METHOD(int8_matmul),
-                          METHOD(linear_forward), METHOD(linear_backward),  METHOD(rms_norm),
-                          METHOD(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef kMethods[] = {METHOD(quantize_rows), METHOD(quantize_cols), METHOD(int8_matmul), METHOD(int8_linear), METHOD(rms_norm),
+                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_operators", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -116,6 +116,8 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   static const char* const call = "prm_quantize_cols";
   TRY(check_type(dtype));
   TRY(check_rows(call, rows, cols, 1, kMaxColRows));
+  if (((cols + 63) / 64) * ((rows + 127) / 128) >= (1ll << 24))  // a grid holds less than 2^32 threads
+    return fail(PRM_EINVAL, "%s: %lld x %lld is too large", call, (long long)rows, (long long)cols);
   TRY(check_ld(call, "ldx", ldx, cols));
   TRY(check_ld(call, "ldq", ldq, rows));
   TRY(check_workspace(call, workspace, workspace_bytes, prm_quantize_cols_workspace(rows, cols)));
@@ -133,7 +135,11 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   quantize_cols_blocks(rows, cols, &a.nrb, &a.rows_per_block);
   a.part_max = (uint32_t*)workspace;
   a.part_sum = (float*)workspace + (int64_t)a.nrb * cols;
-  return launched(call, launch_quantize_cols((OpType)dtype, a, (hipStream_t)hip_stream));
+  QuantJobs jobs = {};
+  jobs.a[0] = a;
+  jobs.columns[0] = true;
+  jobs.n = 1;
+  return launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream));
 }
 
 // prm_int8_matmul; `kind` and `splits`: a ProductPlan, or 0 for the rule's (tests hold
@@ -182,6 +188,157 @@ int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const in
                     void* workspace, uint64_t workspace_bytes, void* hip_stream) {
   return prm_internal_int8_matmul(a, lda, a_scale, b, ldb, b_scale, bias, dtype, out, ldo, m, n, k, workspace,
                                   workspace_bytes, hip_stream, 0, 0);
+}
+
+// The layer's operands in 8 bits, their scales and the statistics' partial sums, one after
+// the other in the caller's workspace (base NULL: their size alone).
+struct Layout {
+  char* base;
+  uint64_t used = 0;
+  void* take(uint64_t bytes) {
+    void* p = base ? base + used : nullptr;
+    used += (bytes + 255) & ~uint64_t(255);
+    return p;
+  }
+};
+// x (rows x cols) by rows or columns; `sum` as in prm_quantize_cols
+static QuantArgs quantiser(Layout& l, const void* x, int64_t rows, int64_t cols, int64_t ldx, bool columns, void* sum) {
+  QuantArgs a = {};
+  a.x = x;
+  a.rows = rows;
+  a.cols = cols;
+  a.ldx = ldx;
+  a.sum = sum;
+  const int64_t out_rows = columns ? cols : rows, out_cols = columns ? rows : cols;
+  a.ldq = (out_cols + 15) / 16 * 16;
+  a.q = (int8_t*)l.take((uint64_t)out_rows * (uint64_t)a.ldq);
+  a.scale = (float*)l.take((uint64_t)out_rows * 4);
+  if (columns) {
+    quantize_cols_blocks(rows, cols, &a.nrb, &a.rows_per_block);
+    a.part_max = (uint32_t*)l.take((uint64_t)a.nrb * (uint64_t)cols * 4);
+    a.part_sum = (float*)l.take((uint64_t)a.nrb * (uint64_t)cols * 4);
+  }
+  return a;
+}
+// p^T q of two quantised operands (k: the length of their rows), split where the rule does
+static ProductArgs product_of(const QuantArgs& p, const QuantArgs& q, int64_t m, int64_t n, int64_t k, const void* bias, void* out,
+                              int64_t ldo, void* part) {
+  return ProductArgs{p.q, q.q, p.scale, q.scale, bias, out, m, n, k, p.ldq, q.ldq, ldo, (int32_t*)part};
+}
+
+struct LinearForward {
+  QuantArgs x, w;
+  void* part;
+  uint64_t bytes;
+  LinearForward(char* base, const void* xp, int64_t ldx, const void* wp, int64_t ldw, int64_t m, int64_t n, int64_t k) {
+    Layout l{base};
+    x = quantiser(l, xp, m, k, ldx, false, nullptr);
+    w = quantiser(l, wp, n, k, ldw, false, nullptr);
+    part = l.take(prm_int8_matmul_workspace(m, n, k));
+    bytes = l.used;
+  }
+};
+struct LinearBackward {
+  QuantArgs g, wt, gt, xt;
+  void* part;
+  uint64_t bytes;
+  LinearBackward(char* base, const void* gp, int64_t ldg, const void* xp, int64_t ldx, const void* wp, int64_t ldw, int64_t m,
+                 int64_t n, int64_t k, void* db) {
+    Layout l{base};
+    g = quantiser(l, gp, m, n, ldg, false, nullptr);
+    wt = quantiser(l, wp, n, k, ldw, true, nullptr);
+    gt = quantiser(l, gp, m, n, ldg, true, db);
+    xt = quantiser(l, xp, m, k, ldx, true, nullptr);
+    const uint64_t a = prm_int8_matmul_workspace(m, k, n), b = prm_int8_matmul_workspace(n, k, m);
+    part = l.take(a > b ? a : b);  // the products run one after the other
+    bytes = l.used;
+  }
+};
+static int check_layer(const char* call, int64_t m, int64_t n, int64_t k) {
+  if (m < 0 || n < 1 || k < 1 || m > kMaxProductK || n > kMaxProductK || k > kMaxProductK)
+    return fail(PRM_EINVAL, "%s: invalid sizes m %lld, n %lld, k %lld (at most %lld)", call, (long long)m, (long long)n,
+                (long long)k, (long long)kMaxProductK);
+  return PRM_OK;
+}
+static bool layer_sizes(int64_t m, int64_t n, int64_t k) {
+  return m >= 1 && n >= 1 && k >= 1 && m <= kMaxProductK && n <= kMaxProductK && k <= kMaxProductK;
+}
+
+uint64_t prm_int8_linear_workspace(int64_t m, int64_t n, int64_t k) {
+  return layer_sizes(m, n, k) ? LinearForward(nullptr, nullptr, 0, nullptr, 0, m, n, k).bytes : 0;
+}
+
+int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, int32_t dtype, void* y,
+                    int64_t ldy, int64_t m, int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes,
+                    void* hip_stream) {
+  static const char* const call = "prm_int8_linear";
+  TRY(check_type(dtype));
+  TRY(check_layer(call, m, n, k));
+  TRY(check_ld(call, "ldx", ldx, k));
+  TRY(check_ld(call, "ldw", ldw, k));
+  TRY(check_ld(call, "ldy", ldy, n));
+  if (m == 0) return PRM_OK;
+  const LinearForward f((char*)workspace, x, ldx, w, ldw, m, n, k);
+  TRY(check_workspace(call, workspace, workspace_bytes, f.bytes));
+  const int64_t es = size_of(dtype);
+  TRY(check_buffers(call, {{x, "x", es}, {w, "w", es}, optional(bias, "bias", es), {y, "y", es}, {workspace, "workspace", 16}}));
+  QuantJobs jobs = {};
+  jobs.a[0] = f.x;
+  jobs.a[1] = f.w;
+  jobs.n = 2;
+  TRY(launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream)));
+  const ProductArgs p = product_of(f.x, f.w, m, n, k, bias, y, ldy, f.part);
+  return launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), (hipStream_t)hip_stream));
+}
+
+uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
+  return layer_sizes(m, n, k) ? LinearBackward(nullptr, nullptr, 0, nullptr, 0, nullptr, 0, m, n, k, nullptr).bytes : 0;
+}
+
+int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                             int32_t dtype, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, int64_t m, int64_t n,
+                             int64_t k, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  static const char* const call = "prm_int8_linear_backward";
+  TRY(check_type(dtype));
+  TRY(check_layer(call, m, n, k));
+  if (m == 0) return fail(PRM_EINVAL, "%s: m is 0", call);
+  TRY(check_ld(call, "ldgy", ldgy, n));
+  if (dw) {
+    TRY(check_ld(call, "ldx", ldx, k));
+    TRY(check_ld(call, "lddw", lddw, k));
+  }
+  if (dx) {
+    TRY(check_ld(call, "ldw", ldw, k));
+    TRY(check_ld(call, "lddx", lddx, k));
+  }
+  if (!dx && !dw && !db) return PRM_OK;
+  const LinearBackward f((char*)workspace, gy, ldgy, x, ldx, w, ldw, m, n, k, db);
+  TRY(check_workspace(call, workspace, workspace_bytes, f.bytes));
+  const int64_t es = size_of(dtype);
+  TRY(check_buffers(call, {{gy, "gy", es}, Buf{x, dw ? "x" : nullptr, es}, Buf{w, dx ? "w" : nullptr, es}, optional(dx, "dx", es),
+                           optional(dw, "dw", es), optional(db, "db", es), {workspace, "workspace", 16}}));
+  QuantJobs jobs = {};
+  const auto add = [&](const QuantArgs& a, bool columns) {
+    jobs.columns[jobs.n] = columns;
+    jobs.a[jobs.n++] = a;
+  };
+  if (dx) {
+    add(f.g, false);
+    add(f.wt, true);
+  }
+  if (dw || db) add(f.gt, true);
+  if (dw) add(f.xt, true);
+  hipStream_t s = (hipStream_t)hip_stream;
+  TRY(launched(call, launch_quantize((OpType)dtype, jobs, s)));
+  if (dx) {
+    const ProductArgs p = product_of(f.g, f.wt, m, k, n, nullptr, dx, lddx, f.part);
+    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), s)));
+  }
+  if (dw) {
+    const ProductArgs p = product_of(f.gt, f.xt, n, k, m, nullptr, dw, lddw, f.part);
+    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), s)));
+  }
+  return PRM_OK;
 }
 
 int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w, int32_t dtype,

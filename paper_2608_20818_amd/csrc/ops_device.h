@@ -147,7 +147,7 @@ struct Eight {
   U top;      // max |u| of the row
   float inv;  // 0: every q is 0 (a row of zeros, or one with a value that is not finite)
   bool fp32;  // fp32 decides: always (VALUES), or where it can
-  __device__ __forceinline__ Eight() {}
+  Eight() = default;
   __device__ __forceinline__ explicit Eight(U t) : top(t) {
     fp32 = t > (U)1e-35f && t < (U)3e38f;
     inv = fp32 ? 127.f / (float)t : 0.f;

@@ -41,7 +41,15 @@ struct QuantArgs {
   int32_t nrb, rows_per_block;
 };
 hipError_t launch_quantize_rows(OpType t, const QuantArgs& a, hipStream_t s);
-hipError_t launch_quantize_cols(OpType t, const QuantArgs& a, hipStream_t s);
+// Up to four quantisers of one type, by rows or (`columns`) by columns, in one launch for
+// rows and the columns' statistics and one for the columns.
+struct QuantJobs {
+  QuantArgs a[4];
+  bool columns[4];
+  int32_t blocks[4];  // of a launch, laid out by it
+  int32_t n;
+};
+hipError_t launch_quantize(OpType t, const QuantJobs& jobs, hipStream_t s);
 // row blocks of the columns' statistics
 void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block);
 

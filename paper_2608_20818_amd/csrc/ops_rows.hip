@@ -451,14 +451,18 @@ hipError_t launch_grad(const NormGradArgs& a, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // Largest magnitudes (as bits) and sums of the columns over a block of rows: 32 lanes
 // of 8 columns, 8 rows at a time.
+struct ColStatsShared {
+  uint32_t rm[8][256];
+  float rs[8][256];
+};
 template <class E, bool SUM>
-__global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
+__device__ __forceinline__ void col_stats(const QuantArgs& a, int bx, int by, ColStatsShared& sh) {
   using S = typename E::S;
-  __shared__ uint32_t rm[8][256];
-  __shared__ float rs[SUM ? 8 : 1][256];
+  auto& rm = sh.rm;
+  auto& rs = sh.rs;
   const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 256 + 8 * tc;
-  const int64_t r0 = (int64_t)blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const int64_t c = (int64_t)bx * 256 + 8 * tc;
+  const int64_t r0 = (int64_t)by * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   uint32_t m[8];
   float sum[8];
 #pragma unroll
@@ -489,7 +493,7 @@ __global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
     if (SUM) rs[tr][8 * tc + k] = sum[k];
   }
   __syncthreads();
-  const int64_t cc = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t cc = (int64_t)bx * 256 + threadIdx.x;
   if (cc >= a.cols) return;
   uint32_t top = 0;
   float s = 0.f;
@@ -498,23 +502,31 @@ __global__ __launch_bounds__(256) void col_stats_kernel(QuantArgs a) {
     top = max(top, rm[i][threadIdx.x]);
     if (SUM) s += rs[i][threadIdx.x];
   }
-  a.part_max[(int64_t)blockIdx.y * a.cols + cc] = top;
-  if (SUM) a.part_sum[(int64_t)blockIdx.y * a.cols + cc] = s;
+  a.part_max[(int64_t)by * a.cols + cc] = top;
+  if (SUM) a.part_sum[(int64_t)by * a.cols + cc] = s;
 }
 
 // A tile of 128 rows x 64 columns: a thread quantises 4 rows of 8 columns, and the tile
 // leaves through shared memory as 128 bytes of each of its columns, 8 lanes a column.
+template <class E>
+struct ColQuantShared {
+  static constexpr int LD = 33;  // words of a column: rows and columns on distinct banks
+  uint32_t tile[64 * LD];
+  uint32_t pm[4][64];
+  float ps[4][64];
+  EightOf<E> eights[64];
+};
 template <class E, bool SUM>
-__global__ __launch_bounds__(256) void col_quant_kernel(QuantArgs a) {
+__device__ __forceinline__ void col_quant(const QuantArgs& a, int64_t bx, int64_t by, ColQuantShared<E>& sh) {
   using S = typename E::S;
-  constexpr int LD = 33;  // words of a column in shared memory: rows and columns on distinct banks
-  __shared__ uint32_t tile[64 * LD];
-  __shared__ uint32_t pm[4][64];
-  __shared__ float ps[SUM ? 4 : 1][64];
   using E8 = EightOf<E>;
-  __shared__ E8 eights[64];
-  const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
-  const bool first = blockIdx.y == 0;
+  constexpr int LD = ColQuantShared<E>::LD;
+  auto& tile = sh.tile;
+  auto& pm = sh.pm;
+  auto& ps = sh.ps;
+  auto& eights = sh.eights;
+  const int64_t c0 = bx * 64, r0 = by * 128;
+  const bool first = by == 0;
   const int tc = threadIdx.x & 7, tr = threadIdx.x >> 3;
   const int64_t c = c0 + 8 * tc;
   // the tile is on its way while the columns' statistics are joined
@@ -584,16 +596,125 @@ __global__ __launch_bounds__(256) void col_quant_kernel(QuantArgs a) {
   }
 }
 
-template <class E>
-hipError_t launch_cols(const QuantArgs& a, hipStream_t s) {
-  const dim3 g1((unsigned)((a.cols + 255) / 256), (unsigned)a.nrb);
-  const dim3 g2((unsigned)((a.cols + 63) / 64), (unsigned)((a.rows + 127) / 128));
-  if (a.sum) {
-    col_stats_kernel<E, true><<<g1, 256, 0, s>>>(a);
-    col_quant_kernel<E, true><<<g2, 256, 0, s>>>(a);
+// ---------------------------------------------------------------------------
+// several quantisers in one launch: what a layer's pass needs of its operands at once.
+// The launches of small matrices, not their bytes, are what such a pass waits for.
+// ---------------------------------------------------------------------------
+// Rows of at most 8 NCH 256 elements (NCH 0: any), a block a row, or a wave where they are
+// short; blocks take rows in turn.
+template <class E, int NCH>
+__device__ __forceinline__ void quant_rows(const QuantArgs& a, int64_t block, int64_t blocks, uint32_t* red) {
+  using S = typename E::S;
+  constexpr int N = NCH ? NCH : 1;
+  const bool wide = a.cols > 512;
+  const int width = wide ? 256 : 64, t = wide ? threadIdx.x : threadIdx.x & 63;
+  const int64_t cols = a.cols, step = wide ? blocks : 4 * blocks;
+  for (int64_t row = wide ? block : 4 * block + (threadIdx.x >> 6); row < a.rows; row += step) {
+    const S* x = (const S*)a.x + row * a.ldx;
+    typename E::Raw held[N];
+    TopRaw<E> top;
+    if constexpr (NCH) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * width + t);
+        if (c < cols) held[i] = load_row8<E>(x, c, cols);
+      }
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        if (8 * ((int64_t)i * width + t) < cols) top.add(held[i]);
+    } else {
+      for (int64_t c = 8 * t; c < cols; c += 8 * width) top.add(load_row8<E>(x, c, cols));
+    }
+    uint32_t m = wave_max(top.bits());
+    if (wide) {
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+      __syncthreads();
+      m = max(max(red[0], red[1]), max(red[2], red[3]));
+    }
+    const EightOf<E> e(__uint_as_float(m));
+    if (t == 0) a.scale[row] = e.scale(1.f);
+    auto out = [&](int64_t c, const typename E::Raw& raw) __attribute__((always_inline)) {
+      float v[8];
+      E::expand(raw, v);
+      store_q8(a.q + row * a.ldq, c, cols, eight8(e, v));
+    };
+    if constexpr (NCH) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * width + t);
+        if (c < cols) out(c, held[i]);
+      }
+    } else {
+      for (int64_t c = 8 * t; c < cols; c += 8 * width) out(c, load_row8<E>(x, c, cols));
+    }
+    if (wide) __syncthreads();  // the next row's maxima go where this one's were
+  }
+}
+
+template <class E, int NCH>
+__global__ __launch_bounds__(256) void quant_first_kernel(QuantJobs jobs) {
+  __shared__ union {
+    uint32_t red[4];
+    ColStatsShared stats;
+  } sh;
+  int j = 0, b = blockIdx.x;
+  while (j + 1 < jobs.n && b >= jobs.blocks[j]) b -= jobs.blocks[j++];
+  const QuantArgs& a = jobs.a[j];
+  if (!jobs.columns[j]) {
+    quant_rows<E, NCH>(a, b, jobs.blocks[j], sh.red);
   } else {
-    col_stats_kernel<E, false><<<g1, 256, 0, s>>>(a);
-    col_quant_kernel<E, false><<<g2, 256, 0, s>>>(a);
+    const int gx = (int)((a.cols + 255) / 256);
+    if (a.sum) col_stats<E, true>(a, b % gx, b / gx, sh.stats);
+    else col_stats<E, false>(a, b % gx, b / gx, sh.stats);
+  }
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void quant_columns_kernel(QuantJobs jobs) {
+  __shared__ ColQuantShared<E> sh;
+  int j = 0, b = blockIdx.x;
+  while (j + 1 < jobs.n && b >= jobs.blocks[j]) b -= jobs.blocks[j++];
+  const QuantArgs& a = jobs.a[j];
+  const int gx = (int)((a.cols + 63) / 64);
+  if (a.sum) col_quant<E, true>(a, b % gx, b / gx, sh);
+  else col_quant<E, false>(a, b % gx, b / gx, sh);
+}
+
+template <class E>
+hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
+  QuantJobs first = jobs, second = {};
+  int64_t blocks = 0, pieces = 0;
+  for (int j = 0; j < jobs.n; ++j) {
+    const QuantArgs& a = jobs.a[j];
+    int64_t n;
+    if (jobs.columns[j]) {
+      n = (a.cols + 255) / 256 * a.nrb;
+      const int k = second.n++;
+      second.a[k] = a;
+      second.blocks[k] = (int32_t)((a.cols + 63) / 64 * ((a.rows + 127) / 128));
+    } else {
+      n = a.cols > 512 ? a.rows : (a.rows + 3) / 4;
+      n = n < (1 << 20) ? n : 1 << 20;
+      const int64_t p = (a.cols + 7) / 8, per = a.cols > 512 ? (p + 255) / 256 : 1;
+      pieces = per > pieces ? per : pieces;
+    }
+    first.blocks[j] = (int32_t)n;
+    blocks += n;
+  }
+  if (blocks > 0) {
+    const unsigned g = (unsigned)blocks;
+    if (pieces <= 1) quant_first_kernel<E, 1><<<g, 256, 0, s>>>(first);
+    else if (pieces <= 2) quant_first_kernel<E, 2><<<g, 256, 0, s>>>(first);
+    else if (pieces <= 4) quant_first_kernel<E, 4><<<g, 256, 0, s>>>(first);
+    else if (pieces <= 8) quant_first_kernel<E, 8><<<g, 256, 0, s>>>(first);
+    else quant_first_kernel<E, 0><<<g, 256, 0, s>>>(first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (second.n) {
+    int64_t g = 0;
+    for (int j = 0; j < second.n; ++j) g += second.blocks[j];
+    quant_columns_kernel<E><<<(unsigned)g, 256, 0, s>>>(second);
   }
   return hipGetLastError();
 }
@@ -628,8 +749,8 @@ void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* row
   *nrb = (int32_t)((rows + per - 1) / per);
 }
 
-hipError_t launch_quantize_cols(OpType t, const QuantArgs& a, hipStream_t s) {
-  return t == OP_F32 ? launch_cols<TF32>(a, s) : t == OP_BF16 ? launch_cols<TBF16>(a, s) : launch_cols<TF16>(a, s);
+hipError_t launch_quantize(OpType t, const QuantJobs& jobs, hipStream_t s) {
+  return t == OP_F32 ? launch_jobs<TF32>(jobs, s) : t == OP_BF16 ? launch_jobs<TBF16>(jobs, s) : launch_jobs<TF16>(jobs, s);
 }
 
 // Blocks, each of which leaves a row of partial dw: as many as the card holds at once (of

@@ -22,8 +22,7 @@ try:  # the plain calls, natively where _operators.so is built; None: not a plai
     from . import _operators as _native
 except ImportError:
     class _native:
-        quantize_rows = quantize_cols = int8_matmul = staticmethod(lambda *a: None)
-        rms_norm = rms_norm_backward = linear_forward = linear_backward = staticmethod(lambda *a: None)
+        quantize_rows = quantize_cols = int8_matmul = int8_linear = rms_norm = staticmethod(lambda *a: None)
 
 __all__ = ["quantize_rows", "int8_matmul", "int8_linear", "rms_norm"]
 
@@ -106,6 +105,9 @@ def quantize_rows(x, transpose: bool = False):
     instead, ``q`` is ``[cols, rows]`` and ``scale`` ``[cols]``, what
     ``quantize_rows(x.t())`` gives without a transposed copy.  Not differentiable."""
     if transpose:
+        r = _native.quantize_cols(x)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
         return _quantize_cols(x, False)[:2]
     r = _native.quantize_rows(x)
     if r is not None:
@@ -123,9 +125,6 @@ def quantize_rows(x, transpose: bool = False):
 
 
 def _quantize_cols(x, with_sum):
-    r = _native.quantize_cols(x, with_sum)
-    if r is not None:
-        return r if type(r) is tuple else _check(r)
     _on_device(x, "x")
     code = _float_code(x, "x")
     x = x.detach()
@@ -187,6 +186,30 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     return out
 
 
+# ---- gradients of gradients: refused where they are asked for, and not before --------
+class _Refuse(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, *grads):
+        return tuple(g.detach() for g in grads)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("these gradients are not differentiable")
+
+
+def _once(backward):
+    def wrapped(ctx, *grads):
+        recording = torch.is_grad_enabled()
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not recording:
+            return out
+        kept = [g.detach().requires_grad_() for g in out if g is not None]
+        refusing = iter(_Refuse.apply(*kept)) if kept else iter(())
+        return tuple(None if g is None else next(refusing) for g in out)
+    return wrapped
+
+
 # ---- norm ------------------------------------------------------------------
 def _norm(x, weight, residual, eps, quantize):
     code = _float_code(x, "x")
@@ -218,28 +241,20 @@ def _norm(x, weight, residual, eps, quantize):
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
-        r = _native.rms_norm(x, weight, residual, eps, False, True)
-        if r is None:
-            y, _, _, h = _norm(x, weight, residual, eps, False)
-        else:
-            y, h = (_check(r) if type(r) is int else r) if residual is not None else (r if type(r) is not int else _check(r), None)
+        y, _, _, h = _norm(x, weight, residual, eps, False)
         ctx.save_for_backward(x if h is None else h, weight)
         ctx.eps = eps
         ctx.set_materialize_grads(False)
         return y if h is None else (y, h)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, gy, gh=None):
         h, weight = ctx.saved_tensors
         need_dw = weight is not None and ctx.needs_input_grad[1]
         if gy is None:  # only the kept sum has a gradient
             dw = torch.zeros_like(weight) if need_dw else None
             return (gh if ctx.needs_input_grad[0] else None), dw, (gh if ctx.needs_input_grad[2] else None), None
-        r = _native.rms_norm_backward(gy, gh, h, weight, ctx.eps, need_dw)
-        if r is not None:
-            dx, dw = r if type(r) is tuple else _check(r)
-            return (dx if ctx.needs_input_grad[0] else None), dw, (dx if ctx.needs_input_grad[2] else None), None
         rows, cols = _count(h)
         L = load()
         with _device_of(h) as stream:
@@ -267,7 +282,7 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
     ``residual`` (shaped as x) have x's type.  The plain outputs are differentiable in
     x, weight and residual; the 8-bit ones are not."""
     eps = float(eps)
-    r = _native.rms_norm(x, weight, residual, eps, quantize, False)
+    r = _native.rms_norm(x, weight, residual, eps, quantize)
     if r is not None:
         return _check(r) if type(r) is int else r
     _on_device(x, "x")
@@ -291,27 +306,17 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
 
 
 # ---- linear layer ------------------------------------------------------------
-def _linear(x, weight, bias):
-    r = _native.linear_forward(x, weight, bias)
-    if r is not None:
-        return _check(r) if type(r) is int else r
-    return int8_matmul(*quantize_rows(x), *quantize_rows(weight), bias=bias, dtype=x.dtype)
-
-
 class _Int8Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias):
         ctx.save_for_backward(x, weight)
-        return _linear(x, weight, bias)
+        return int8_matmul(*quantize_rows(x), *quantize_rows(weight), bias=bias, dtype=x.dtype)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, gy):
         x, weight = ctx.saved_tensors
         need_x, need_w, need_b = ctx.needs_input_grad
-        r = _native.linear_backward(gy, x, weight, need_x, need_w, need_b)
-        if r is not None:
-            return r if type(r) is tuple else _check(r)
         g = gy.reshape(-1, gy.shape[-1])
         dx = dw = db = None
         if g.shape[0] == 0:
@@ -337,6 +342,9 @@ def int8_linear(x, weight, bias=None):
     ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T`` (at most 131071 tokens),
     ``dbias`` the sum of ``gy`` in fp32.  Each rounding to 8 bits is off by at most half of
     1/127 of its row's (column's) largest value."""
+    r = _native.int8_linear(x, weight, bias)
+    if r is not None:
+        return _check(r) if type(r) is int else r
     _on_device(x, "x")
     _float_code(x, "x")
     _, k = _count(x)

@@ -585,6 +585,79 @@ def test_linear_gradients_against_the_unquantised_layer():
         check(out, a @ b.t(), bound + 1e-5)
 
 
+@pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("mnk", [(1, 1, 1), (5, 700, 33), (130, 513, 600), (64, 96, 2049), (33, 5000, 70), (40, 17, 20000), (3000, 24, 40)], ids=str)
+def test_linear_is_its_parts(mnk, t):
+    # one call of the layer, and the quantisers and products that it is made of: the same bits
+    m, n, k = mnk
+    x, w, b = rand((m, k), t, 111).cuda(), rand((n, k), t, 112, 0.02).cuda(), rand((n,), t, 113).cuda()
+    gy = rand((m, n), t, 114, 1e-2).cuda()
+    leaves = [v.requires_grad_() for v in (x, w, b)]
+    y = prm.int8_linear(*leaves)
+    got = torch.autograd.grad(y, leaves, gy)
+    with torch.no_grad():
+        assert torch.equal(y, prm.int8_matmul(*prm.quantize_rows(x), *prm.quantize_rows(w), bias=b, dtype=t))
+        assert torch.equal(y, prm.int8_linear(x, w, b))
+        assert torch.equal(got[0], prm.int8_matmul(*prm.quantize_rows(gy), *prm.quantize_rows(w, transpose=True), dtype=t))
+        assert torch.equal(got[1], prm.int8_matmul(*prm.quantize_rows(gy, transpose=True), *prm.quantize_rows(x, transpose=True), dtype=t))
+
+
+@pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
+def test_python_path_is_the_native_one(t, monkeypatch):
+    # the calls that native code leaves to Python, and all of them where it is not built
+    from paper_2608_20818_amd import operators
+    x, res, w = (rand(s, t, 120 + i).cuda().requires_grad_() for i, s in enumerate([(9, 70), (9, 70), (70,)]))
+    wl, b = rand((20, 70), t, 123).cuda().requires_grad_(), rand((20,), t, 124).cuda().requires_grad_()
+    gy = rand((9, 20), t, 125).cuda()
+
+    def run():
+        y, h = prm.rms_norm(x, w, res)
+        z = prm.int8_linear(y, wl, b)
+        out = [y, h, z, *torch.autograd.grad((z, h), (x, res, w, wl, b), (gy, torch.ones_like(h)))]
+        with torch.no_grad():
+            q, s, h8 = prm.rms_norm(x, w, res, quantize=True)
+            out += [q, s, h8, *prm.quantize_rows(wl), *prm.quantize_rows(wl, transpose=True), prm.rms_norm(x),
+                    prm.int8_matmul(q, s, *prm.quantize_rows(wl), bias=b, dtype=t)]
+        return [v.detach() for v in out]
+
+    native = run()
+    monkeypatch.setattr(operators, "_native", type("none", (), {n: staticmethod(lambda *a: None) for n in (
+        "quantize_rows", "quantize_cols", "int8_matmul", "int8_linear", "rms_norm")}))
+    assert all(torch.equal(a, c) for a, c in zip(native, run()))
+
+
+def test_gradients_once():
+    # gradients of gradients are refused, and not before they are asked for
+    for native in (True, False):
+        x, w, wl = (rand(s, torch.float32, 130 + i).cuda().requires_grad_() for i, s in enumerate([(4, 16), (16,), (8, 16)]))
+        xv = x if native else x.as_subclass(type("Sub", (torch.Tensor,), {}))
+        for y, v in ((prm.rms_norm(xv, w), w), (prm.int8_linear(xv, wl), wl)):
+            gx, gv = torch.autograd.grad(y.sum(), (x, v), create_graph=True)
+            assert torch.isfinite(gx).all() and torch.isfinite(gv).all()
+            with pytest.raises(RuntimeError, match="differentia"):
+                torch.autograd.grad(gx.square().sum(), x)
+
+
+def test_saved_tensors_changed_in_place():
+    x, wl = rand((4, 16), torch.float32, 140).cuda().requires_grad_(), rand((8, 16), torch.float32, 141).cuda().requires_grad_()
+    for f in (lambda: prm.int8_linear(x, wl), lambda: prm.rms_norm(x)):
+        y = f()
+        with torch.no_grad():
+            x.add_(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(y.sum(), x)
+
+
+def test_accumulates_into_leaves():
+    # .backward() twice adds, through a parameter used by two layers
+    x, p = rand((6, 32), torch.float32, 142).cuda(), torch.nn.Parameter(rand((32, 32), torch.float32, 143).cuda())
+    y = prm.int8_linear(prm.int8_linear(x, p), p)
+    y.sum().backward()
+    once = p.grad.clone()
+    prm.int8_linear(prm.int8_linear(x, p), p).sum().backward()
+    assert torch.equal(p.grad, once + once)
+
+
 def test_linear_layouts():
     t = torch.bfloat16
     x, w, b = rand((2, 5, 48), t, 58).cuda(), rand((31, 48), t, 59).cuda(), rand((31,), t, 60).cuda()

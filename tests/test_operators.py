@@ -34,7 +34,10 @@ N = dict(x=FAKE, ldx=8, res=None, ldres=0, w=FAKE, dtype=BF, rows=4, cols=8, eps
          ldq=0, scale=None, stream=None)
 G = dict(gy=FAKE, ldgy=8, gh=None, ldgh=0, h=FAKE, ldh=8, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, dx=FAKE, lddx=8,
          dw=FAKE, ws=FAKE, nws=1 << 16, stream=None)
-BASE = {"prm_quantize_rows": Q, "prm_quantize_cols": C, "prm_int8_matmul": M, "prm_rms_norm": N, "prm_rms_norm_backward": G}
+F = dict(x=FAKE, ldx=8, w=FAKE, ldw=8, bias=None, dtype=BF, y=FAKE, ldy=6, m=4, n=6, k=8, ws=FAKE, nws=1 << 20, stream=None)
+B = dict(gy=FAKE, ldgy=6, x=FAKE, ldx=8, w=FAKE, ldw=8, dtype=BF, dx=FAKE, lddx=8, dw=FAKE, lddw=8, db=FAKE, m=4, n=6, k=8, ws=FAKE,
+         nws=1 << 20, stream=None)
+BASE = {"prm_int8_linear": F, "prm_int8_linear_backward": B, "prm_quantize_rows": Q, "prm_quantize_cols": C, "prm_int8_matmul": M, "prm_rms_norm": N, "prm_rms_norm_backward": G}
 
 
 @pytest.mark.parametrize("name", sorted(BASE))
@@ -60,6 +63,14 @@ def test_unknown_type(name):
     ("prm_rms_norm", dict(y=None)), ("prm_rms_norm", dict(q=FAKE, ldq=8)), ("prm_rms_norm", dict(y=None, q=FAKE, ldq=8)),
     ("prm_rms_norm", dict(y=None, q=FAKE, ldq=7, scale=FAKE)), ("prm_rms_norm", dict(ldy=7)), ("prm_rms_norm", dict(cols=0)),
     ("prm_rms_norm", dict(x=None)),
+    ("prm_int8_linear", dict(m=-1)), ("prm_int8_linear", dict(n=0)), ("prm_int8_linear", dict(k=131072, ldx=131072, ldw=131072)),
+    ("prm_int8_linear", dict(m=131072)), ("prm_int8_linear", dict(ldx=7)), ("prm_int8_linear", dict(ldw=7)), ("prm_int8_linear", dict(ldy=5)),
+    ("prm_int8_linear", dict(nws=64)), ("prm_int8_linear", dict(ws=None)), ("prm_int8_linear", dict(w=None)),
+    ("prm_int8_linear_backward", dict(m=0)), ("prm_int8_linear_backward", dict(n=131072, ldgy=131072)),
+    ("prm_int8_linear_backward", dict(ldgy=5)), ("prm_int8_linear_backward", dict(ldx=7)), ("prm_int8_linear_backward", dict(ldw=7)),
+    ("prm_int8_linear_backward", dict(lddx=7)), ("prm_int8_linear_backward", dict(lddw=7)), ("prm_int8_linear_backward", dict(nws=64)),
+    ("prm_int8_linear_backward", dict(x=None)), ("prm_int8_linear_backward", dict(w=None)), ("prm_int8_linear_backward", dict(gy=None)),
+    ("prm_quantize_cols", dict(rows=1 << 22, cols=1 << 16, ldx=1 << 16, ldq=1 << 22, nws=1 << 40)),
     ("prm_rms_norm_backward", dict(eps=-1.0)), ("prm_rms_norm_backward", dict(ldgy=7)),
     ("prm_rms_norm_backward", dict(gh=FAKE, ldgh=7)), ("prm_rms_norm_backward", dict(ldh=7)),
     ("prm_rms_norm_backward", dict(lddx=7)), ("prm_rms_norm_backward", dict(nws=4)),
@@ -86,6 +97,8 @@ def test_nothing_to_do():
     assert L.prm_int8_matmul(*changed(M, n=0)) == prm.PRM_OK
     assert L.prm_rms_norm(*changed(N, rows=0)) == prm.PRM_OK
     assert L.prm_rms_norm_backward(*changed(G, rows=0, dw=None)) == prm.PRM_OK
+    assert L.prm_int8_linear(*changed(F, m=0, x=None, ws=None)) == prm.PRM_OK
+    assert L.prm_int8_linear_backward(*changed(B, dx=None, dw=None, db=None, ws=None)) == prm.PRM_OK
 
 
 def test_workspace_sizes():
@@ -95,6 +108,32 @@ def test_workspace_sizes():
         assert f(1, 1) > 0 and f(8192, 4096) >= 4 * 4096
         assert f(8192, 4096) % 4 == 0
     assert L.prm_quantize_cols_workspace((1 << 22) + 1, 8) == 0
+    for f in (L.prm_int8_linear_workspace, L.prm_int8_linear_backward_workspace):
+        assert f(0, 8, 8) == f(8, 0, 8) == f(8, 8, 0) == f(131072, 8, 8) == 0
+        assert f(100, 60, 30) >= 100 * 30 + 60 * 30
+
+
+def test_16_bit_values_round_right_without_a_check():
+    """The quantiser's claim for values of a 16-bit type: rint of u inv, the product unrounded
+    (an fma), with inv = 127 / top rounded up, is the nearest whole number of 127 u / top,
+    ties to even, for every value u = U 2^-j and top = T whose whole T 127 does not divide."""
+    from fractions import Fraction
+
+    import numpy as np
+    for bits in (8, 11):  # bf16, fp16: whole numbers of that many bits
+        for T in range(1 << (bits - 1), 1 << bits):
+            inv = np.float32(127) / np.float32(T)
+            if Fraction(float(inv)) * T < 127:
+                inv = np.nextafter(inv, np.float32(np.inf))
+            if T % 127 == 0:
+                continue
+            for j in range(9):
+                U = np.arange(1 << (bits - 1), min(T << j, (1 << bits) - 1) + 1, dtype=np.int64)
+                n = np.rint(U * float(inv) / (1 << j)).astype(np.int64)  # 11 + 24 bits: exact in fp64
+                num, den = 254 * U, 2 * (T << j)
+                k = num // den
+                rest = 2 * (num - k * den)
+                assert np.array_equal(n, k + ((rest > den) | ((rest == den) & (k % 2 == 1)))), (bits, T, j)
 
 
 def test_the_step_takes_no_fp16():
