@@ -601,7 +601,7 @@ __device__ __forceinline__ void col_quant(const QuantArgs& a, int64_t bx, int64_
 // The launches of small matrices, not their bytes, are what such a pass waits for.
 // ---------------------------------------------------------------------------
 // Rows of at most 8 NCH 256 elements (NCH 0: any), a block a row, or a wave where they are
-// short; blocks take rows in turn.
+// short; blocks take rows in turn, the next one on its way while one is rounded.
 template <class E, int NCH>
 __device__ __forceinline__ void quant_rows(const QuantArgs& a, int64_t block, int64_t blocks, uint32_t* red) {
   using S = typename E::S;
@@ -609,16 +609,25 @@ __device__ __forceinline__ void quant_rows(const QuantArgs& a, int64_t block, in
   const bool wide = a.cols > 512;
   const int width = wide ? 256 : 64, t = wide ? threadIdx.x : threadIdx.x & 63;
   const int64_t cols = a.cols, step = wide ? blocks : 4 * blocks;
-  for (int64_t row = wide ? block : 4 * block + (threadIdx.x >> 6); row < a.rows; row += step) {
+  typename E::Raw next[N];
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int64_t c = 8 * ((int64_t)i * width + t);
+      if (c < cols) next[i] = load_row8<E>((const S*)a.x + row * a.ldx, c, cols);
+    }
+  };
+  int64_t row = wide ? block : 4 * block + (threadIdx.x >> 6);
+  if (NCH && row < a.rows) fetch(row);
+  int flip = 0;
+  for (; row < a.rows; row += step) {
     const S* x = (const S*)a.x + row * a.ldx;
     typename E::Raw held[N];
     TopRaw<E> top;
     if constexpr (NCH) {
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int64_t c = 8 * ((int64_t)i * width + t);
-        if (c < cols) held[i] = load_row8<E>(x, c, cols);
-      }
+      for (int i = 0; i < NCH; ++i) held[i] = next[i];
+      if (row + step < a.rows) fetch(row + step);
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
         if (8 * ((int64_t)i * width + t) < cols) top.add(held[i]);
@@ -627,9 +636,11 @@ __device__ __forceinline__ void quant_rows(const QuantArgs& a, int64_t block, in
     }
     uint32_t m = wave_max(top.bits());
     if (wide) {
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+      // two sets of slots in turn: a wave writes the next row's behind one barrier only
+      if ((threadIdx.x & 63) == 0) red[flip + (threadIdx.x >> 6)] = m;
       __syncthreads();
-      m = max(max(red[0], red[1]), max(red[2], red[3]));
+      m = max(max(red[flip], red[flip + 1]), max(red[flip + 2], red[flip + 3]));
+      flip ^= 4;
     }
     const EightOf<E> e(__uint_as_float(m));
     if (t == 0) a.scale[row] = e.scale(1.f);
@@ -647,14 +658,13 @@ __device__ __forceinline__ void quant_rows(const QuantArgs& a, int64_t block, in
     } else {
       for (int64_t c = 8 * t; c < cols; c += 8 * width) out(c, load_row8<E>(x, c, cols));
     }
-    if (wide) __syncthreads();  // the next row's maxima go where this one's were
   }
 }
 
 template <class E, int NCH>
 __global__ __launch_bounds__(256) void quant_first_kernel(QuantJobs jobs) {
   __shared__ union {
-    uint32_t red[4];
+    uint32_t red[8];
     ColStatsShared stats;
   } sh;
   int j = 0, b = blockIdx.x;
@@ -680,10 +690,17 @@ __global__ __launch_bounds__(256) void quant_columns_kernel(QuantJobs jobs) {
   else col_quant<E, false>(a, b % gx, b / gx, sh);
 }
 
+// Blocks that take rows: eight a CU, as many as it holds.
+constexpr int64_t kRowBlocks = 2048;
+
 template <class E>
 hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
   QuantJobs first = jobs, second = {};
-  int64_t blocks = 0, pieces = 0;
+  int64_t blocks = 0, pieces = 0, rows = 0;
+  const auto groups = [](const QuantArgs& a) { return a.cols > 512 ? a.rows : (a.rows + 3) / 4; };
+  for (int j = 0; j < jobs.n; ++j)
+    if (!jobs.columns[j]) rows += groups(jobs.a[j]);
+  const int64_t per_block = (rows + kRowBlocks - 1) / kRowBlocks;
   for (int j = 0; j < jobs.n; ++j) {
     const QuantArgs& a = jobs.a[j];
     int64_t n;
@@ -693,8 +710,7 @@ hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
       second.a[k] = a;
       second.blocks[k] = (int32_t)((a.cols + 63) / 64 * ((a.rows + 127) / 128));
     } else {
-      n = a.cols > 512 ? a.rows : (a.rows + 3) / 4;
-      n = n < (1 << 20) ? n : 1 << 20;
+      n = (groups(a) + per_block - 1) / per_block;
       const int64_t p = (a.cols + 7) / 8, per = a.cols > 512 ? (p + 255) / 256 : 1;
       pieces = per > pieces ? per : pieces;
     }
@@ -739,11 +755,13 @@ hipError_t launch_quantize_rows(OpType t, const QuantArgs& q, hipStream_t s) {
                         : launch_rows<TF16, QUANT, false>(a, s);
 }
 
-// At most 64 row blocks of at least 64 rows each: the second kernel's blocks each read
-// them all.
+// Row blocks of the columns' statistics: of at least 64 rows, at most 64, and no more than
+// fill the card (kStatBlocks of 256 columns), as each tile of the second kernel reads the
+// statistics of all.
+constexpr int64_t kStatBlocks = 1024;  // 8192 x 16384 bf16: 135 us; 512 135, 2048 139, no bound 148
 void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block) {
-  (void)cols;
-  int64_t per = (rows + 63) / 64;
+  const int64_t most = kStatBlocks / ((cols + 255) / 256), n = most < 1 ? 1 : most > 64 ? 64 : most;
+  int64_t per = (rows + n - 1) / n;
   per = per < 64 ? 64 : per;
   *rows_per_block = (int32_t)per;
   *nrb = (int32_t)((rows + per - 1) / per);
