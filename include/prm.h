@@ -357,13 +357,14 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
 
 /* out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] b[j][k] + bias[j], for a
  * (m x k: tokens), b (n x k: output channels, as a linear layer's weight is kept)
- * and out (m x n, type dtype).  The sum is exact (32-bit whole numbers: 1 <= k <=
- * 131071, where 128 * 128 k still fits), the rest fp32, rounded once.  bias: n values
- * of type dtype, or NULL.  0 <= m, n <= 2^24.  Operands whose rows start on 16-byte
+ * and out (m x n, type dtype).  The sum is exact (whole numbers), the rest fp32, rounded
+ * once.  1 <= k <= 2^20; over 131071, where 128 * 128 k passes 32 bits, the operands' rows
+ * have to start on 16-byte boundaries and the workspace has to be there (PRM_EINVAL).
+ * bias: n values of type dtype, or NULL.  0 <= m, n <= 2^24.  Operands whose rows start on 16-byte
  * boundaries (a and b, lda and ldb) take faster loads.  `workspace`:
  * prm_int8_matmul_workspace(m, n, k) bytes (0 for most sizes), 16-byte aligned, used by
  * this call only; a product with few outputs and a long sum is split there.  With less,
- * or NULL, it is not split: the same result, later. */
+ * or NULL, one of k <= 131071 is not split: the same result, later. */
 uint64_t prm_int8_matmul_workspace(int64_t m, int64_t n, int64_t k);
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
                     const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo,
@@ -372,7 +373,7 @@ int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const in
 
 /* A linear layer with its products in 8 bits: y = Q(x) Q(w)^T + bias, for x (m x k), w
  * (n x k), bias (n values, or NULL) and y (m x n), all of type dtype; Q quantises each
- * row as prm_quantize_rows does.  m, n, k <= 131071.  What prm_quantize_rows of x and
+ * row as prm_quantize_rows does.  m, n, k <= 2^20.  What prm_quantize_rows of x and
  * of w and prm_int8_matmul give, bit for bit, in fewer launches.  `workspace`:
  * prm_int8_linear_workspace(m, n, k) bytes, 16-byte aligned, used by this call only. */
 uint64_t prm_int8_linear_workspace(int64_t m, int64_t n, int64_t k);

@@ -47,8 +47,8 @@ at::ScalarType type_of(long code) {
   return code == PRM_F32 ? at::kFloat : code == PRM_BF16 ? at::kBFloat16 : code == PRM_F16 ? at::kHalf : at::ScalarType::Undefined;
 }
 
-// The last dimension's rows as a matrix without a copy: 2-D with contiguous rows, or
-// contiguous as a whole.
+// The last dimension's rows as a matrix without a copy: contiguous rows, evenly spaced
+// over all leading dimensions.
 struct Rows {
   int64_t rows = 0, cols = 0, ld = 0;
 };
@@ -58,12 +58,17 @@ bool rows_of(const at::Tensor& t, Rows* r) {
   r->cols = t.size(d - 1);
   if (r->cols < 1 || t.numel() == 0) return false;
   r->rows = t.numel() / r->cols;
-  if (d == 2 && (t.stride(1) == 1 || r->cols == 1) && (t.stride(0) >= r->cols || r->rows == 1)) {
-    r->ld = r->rows == 1 ? r->cols : t.stride(0);
-    return true;
+  if (r->cols > 1 && t.stride(d - 1) != 1) return false;
+  int64_t rows = 1, step = 0;  // rows of the inner dimensions, and how far apart
+  for (int64_t i = d - 2; i >= 0; --i) {
+    if (t.size(i) == 1) continue;
+    if (rows == 1) step = t.stride(i);
+    else if (t.stride(i) != rows * step) return false;
+    rows *= t.size(i);
   }
-  r->ld = r->cols;
-  return t.is_contiguous();
+  if (rows > 1 && step < r->cols) return false;
+  r->ld = rows > 1 ? step : r->cols;
+  return true;
 }
 bool vector_of(const at::Tensor& t, const at::Tensor& like, at::ScalarType type, int64_t n) {
   return t.dim() == 1 && t.size(0) == n && t.scalar_type() == type && t.device() == like.device() && (n <= 1 || t.stride(0) == 1);

@@ -161,8 +161,10 @@ int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale,
   ProductPlan plan = {(ProductKind)kind, splits};
   if (kind == 0) {
     plan = product_plan(p);
+    if (!product_takes(p, plan))
+      return fail(PRM_EINVAL, "%s: sums over more than %lld need rows on 16-byte boundaries", call, (long long)kMaxPieceK);
     // without the room that a split needs, the same sums in one piece
-    if (!workspace || workspace_bytes < product_workspace(m, n, plan.splits)) plan.splits = 1;
+    if (k <= kMaxPieceK && (!workspace || workspace_bytes < product_workspace(m, n, plan.splits))) plan.splits = 1;
   } else if (kind < 0 || kind >= PRODUCT_KINDS || !product_takes(p, plan)) {
     return fail(PRM_EINVAL, "%s: kernel %d does not take this product in %d", call, kind, splits);
   }
@@ -254,14 +256,14 @@ struct LinearBackward {
     bytes = l.used;
   }
 };
+static bool layer_sizes(int64_t m, int64_t n, int64_t k) {
+  return m >= 1 && n >= 1 && k >= 1 && m <= kMaxProductK && n <= kMaxProductK && k <= kMaxProductK;
+}
 static int check_layer(const char* call, int64_t m, int64_t n, int64_t k) {
-  if (m < 0 || n < 1 || k < 1 || m > kMaxProductK || n > kMaxProductK || k > kMaxProductK)
+  if (m != 0 && !layer_sizes(m, n, k))
     return fail(PRM_EINVAL, "%s: invalid sizes m %lld, n %lld, k %lld (at most %lld)", call, (long long)m, (long long)n,
                 (long long)k, (long long)kMaxProductK);
   return PRM_OK;
-}
-static bool layer_sizes(int64_t m, int64_t n, int64_t k) {
-  return m >= 1 && n >= 1 && k >= 1 && m <= kMaxProductK && n <= kMaxProductK && k <= kMaxProductK;
 }
 
 uint64_t prm_int8_linear_workspace(int64_t m, int64_t n, int64_t k) {

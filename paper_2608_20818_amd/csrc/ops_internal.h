@@ -93,6 +93,8 @@ bool product_takes(const ProductArgs& p, const ProductPlan& plan);
 ProductPlan product_plan(const ProductArgs& p);  // the rule
 uint64_t product_workspace(int64_t m, int64_t n, int32_t splits);
 hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, const ProductPlan& plan, hipStream_t s);
-constexpr int64_t kMaxProductK = 131071;  // 128 * 128 * k stays below 2^31
+// 128 * 128 k stays below 2^31 in one piece; longer sums are split and joined in 64 bits
+constexpr int64_t kMaxPieceK = 131071, kMaxProductK = 1 << 20;
+constexpr int64_t kMaxTiles = 1 << 24;  // a grid holds less than 2^32 threads
 
 }  // namespace prm

@@ -579,25 +579,30 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(ProductArgs p) {
   store4<E>((typename E::S*)p.out + r * p.ldo, c, p.n, v);
 }
 
-// The sums of the splits, joined and scaled: 8 columns a thread.
+// The sums of the splits, joined (in 64 bits: a sum longer than one piece may pass 2^31) and
+// scaled: 8 columns a thread.
 template <class E>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs p, int splits) {
   const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x, per = (p.n + 7) / 8;
   const int64_t row = piece / per, c = 8 * (piece - row * per);
   if (row >= p.m) return;
   const int64_t ldp = 8 * per;
-  i32x4_t lo = {}, hi = {};
+  int64_t sum[8] = {};
   for (int s = 0; s < splits; ++s) {
     const PRM_GLOBAL i32x4_t* src = (const PRM_GLOBAL i32x4_t*)(p.part + ((int64_t)s * p.m + row) * ldp + c);
-    lo += src[0];
-    hi += src[1];
+    const i32x4_t lo = src[0], hi = src[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sum[e] += lo[e];
+      sum[4 + e] += hi[e];
+    }
   }
   const float as = *gptr(p.a_scale + row);
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int64_t cc = min(c + e, p.n - 1);
-    v[e] = (float)(e < 4 ? lo[e & 3] : hi[e & 3]) * as * *gptr(p.b_scale + cc);
+    v[e] = (float)sum[e] * as * *gptr(p.b_scale + cc);
     if (p.bias) v[e] += E::load1((const typename E::S*)p.bias + cc);
   }
   store_row8<E>((typename E::S*)p.out + row * p.ldo, c, p.n, E::pack(v));
@@ -618,6 +623,7 @@ template <class E>
 hipError_t launch(const ProductArgs& p, const ProductPlan& plan, hipStream_t s) {
   const int64_t b = plan.kind == PRODUCT_256 ? 256 : plan.kind == PRODUCT_ANY64 ? 64 : 128;
   const int64_t tm = (p.m + b - 1) / b, tn = (p.n + b - 1) / b;
+  if (tm * tn >= kMaxTiles) return hipErrorInvalidValue;
   const unsigned tiles = (unsigned)(tm * tn);
   switch (plan.kind) {
     case PRODUCT_FEW: few_kernel<E, 8><<<(unsigned)((p.n + 15) / 16), 512, 0, s>>>(p); break;
@@ -636,6 +642,8 @@ hipError_t launch(const ProductArgs& p, const ProductPlan& plan, hipStream_t s) 
 bool product_takes(const ProductArgs& p, const ProductPlan& plan) {
   const ProductKind kind = plan.kind;
   const int64_t pieces = p.k / 128;
+  if (plan.splits == 1 ? p.k > kMaxPieceK : plan.splits > 1 && ((pieces + plan.splits - 1) / plan.splits + 1) * 128 > kMaxPieceK)
+    return false;  // a piece's sum has to fit 32 bits
   if (plan.splits != 1 && (kind < PRODUCT_64 || kind == PRODUCT_256 || plan.splits < 1 || plan.splits > pieces || plan.splits > 64))
     return false;
   if (kind == PRODUCT_FEW) return p.m <= 16;
@@ -664,9 +672,11 @@ uint64_t product_workspace(int64_t m, int64_t n, int32_t splits) {
 // 64 x 4096 x 16384 takes 37.7 us in one piece (64), 21.6 in 4; 1024 x 1024 x 65536
 // 147 (64) and 99 (128 in 4); 64 x 4096 x 4096 9.4, and 10.7 in 2.
 ProductPlan product_plan(const ProductArgs& p) {
-  if (p.m <= 8) return {PRODUCT_FEW, 1};
+  if (p.m <= 8 && p.k <= kMaxPieceK) return {PRODUCT_FEW, 1};
   const auto tiles = [&](int64_t b) { return (double)((p.m + b - 1) / b) * (double)((p.n + b - 1) / b); };
-  if (!product_takes(p, {PRODUCT_256, 1})) {
+  ProductArgs q = p;
+  q.k = 128;  // the rows' alignment alone
+  if (!product_takes(q, {PRODUCT_256, 1})) {
     if (p.m <= 16) return {PRODUCT_FEW, 1};
     // rows that start anywhere: 4096 x 4096 x 4097 takes 229 us on 64, 146 on 128;
     // 777 x 1011 x 1357 (56 tiles of 128) 11 and 27
@@ -675,14 +685,15 @@ ProductPlan product_plan(const ProductArgs& p) {
   const double stages = (double)((p.k + 127) / 128);
   const auto rounds = [](double t, double at_once) { return std::ceil(t / at_once); };
   const auto fill = [](double t) { return t < 256 ? t / 256 : 1.0; };
-  double best = 14 + rounds(tiles(256), 256) * (stages * (0.95 + 0.6 * fill(tiles(256))) + 9) - 9;
-  ProductPlan plan = {PRODUCT_256, 1};
+  double best = 1e30;
+  ProductPlan plan = {PRODUCT_64, 64};
   const auto take = [&](ProductKind kind, int splits, double t) {
-    if (t < best) {
+    if (t < best && product_takes(p, {kind, splits})) {
       best = t;
       plan = {kind, splits};
     }
   };
+  take(PRODUCT_256, 1, 14 + rounds(tiles(256), 256) * (stages * (0.95 + 0.6 * fill(tiles(256))) + 9) - 9);
   take(PRODUCT_128_PAIRED, 1, 4 + rounds(tiles(128), 512) * (stages * 1.15 + 4));
   for (int s = 1; s == 1 || (s <= 16 && stages >= 8 * s); s *= 2) {
     const double n = std::ceil(stages / s);

@@ -148,7 +148,8 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     """``a_scale a (b_scale b)^T + bias``: the product of 8-bit operands, ``a``
     ``[..., k]`` with a scale for each row (token) and ``b`` ``[n, k]`` with one for each
     row (output channel, as a linear layer's weight is kept); ``bias`` ``[n]`` and the
-    result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 131071) is exact;
+    result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 2^20; over 131071, of
+    rows on 16-byte boundaries, as ``quantize_rows`` gives them) is exact;
     scales and bias are applied in fp32 and the result rounded once.  Not
     differentiable (``int8_linear`` is)."""
     r = _native.int8_matmul(a, a_scale, b, b_scale, bias, _CODE.get(dtype, -1))
@@ -339,7 +340,7 @@ def int8_linear(x, weight, bias=None):
     each token, ``weight`` ``[n, k]`` for each output channel, all of one type, which the
     result ``[..., n]`` has.  Its gradients are those of the unquantised layer, their
     products in 8 bits too, each operand quantised along the sum it enters:
-    ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T`` (at most 131071 tokens),
+    ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T`` (at most 2^20 tokens),
     ``dbias`` the sum of ``gy`` in fp32.  Each rounding to 8 bits is off by at most half of
     1/127 of its row's (column's) largest value."""
     r = _native.int8_linear(x, weight, bias)
@@ -351,6 +352,8 @@ def int8_linear(x, weight, bias=None):
     if weight.dim() != 2:
         raise ValueError(f"weight: need a matrix, got {tuple(weight.shape)}")
     n = weight.shape[0]
+    if n < 1:
+        raise ValueError("weight: need one output or more")
     _same(weight, x, (n, k), "weight")
     if bias is not None:
         _same(bias, x, (n,), "bias")

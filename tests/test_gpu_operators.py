@@ -324,6 +324,64 @@ def test_product_longest_sum(m, k):
     assert (got.double().cpu() == float(torch.tensor(16384.0 * k, dtype=torch.float32))).all()
 
 
+@pytest.mark.parametrize("m,k", [(1, 131072), (3, 300000), (200, 262161), (70, 1 << 20)])
+def test_product_of_sums_past_32_bits(m, k):
+    # split, and joined in 64 bits; each term 2^14, so the sum in fp32 is off by its own rounding
+    n, ld = 40, (k + 15) // 16 * 16
+    a, b = (torch.full((r, ld), -128, dtype=torch.int8, device="cuda")[:, :k] for r in (m, n))
+    one = torch.ones(max(m, n), device="cuda")
+    got = prm.int8_matmul(a, one[:m], b, one[:n], dtype=torch.float32)
+    assert (got.double() == float(torch.tensor(16384.0 * k, dtype=torch.float32))).all()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    a.copy_(torch.randint(-128, 128, (m, k), dtype=torch.int8, device="cuda", generator=g))
+    b.copy_(torch.randint(-128, 128, (n, k), dtype=torch.int8, device="cuda", generator=g))
+    got = prm.int8_matmul(a, one[:m], b, one[:n], dtype=torch.float32)
+    assert torch.equal(got, (a.double() @ b.double().t()).float())
+    if k % 16:
+        with pytest.raises(prm.PRMError):
+            prm.int8_matmul(a.contiguous(), one[:m], b, one[:n])
+
+
+def test_offsets_past_32_bits():
+    # matrices of more than 2^32 bytes, and of more than 2^31 elements: their last rows
+    t, rows, cols = torch.bfloat16, 70000, 32768
+    x = torch.zeros(rows, cols, dtype=t, device="cuda")
+    end = rand((40, cols), t, 150)
+    x[-40:] = end.cuda()
+    w = rand((cols,), t, 151)
+    qe, se = eight(end.double())
+    q, s = prm.quantize_rows(x)
+    assert torch.equal(q[-40:].cpu().double(), qe) and (q[:-40] == 0).all() and (s[:-40] == 0).all()
+    check_scale(s[-40:], se)
+    y = prm.rms_norm(x, w.cuda())
+    assert torch.equal(y[-40:], prm.rms_norm(end.cuda(), w.cuda()))
+    del y
+    a, sa = int8s((20, cols), 152).cuda(), scales(20, 153).cuda()
+    out = prm.int8_matmul(a, sa, q, s, dtype=torch.float32)
+    assert torch.equal(out[:, -40:], prm.int8_matmul(a, sa, q[-40:].clone(), s[-40:].clone(), dtype=torch.float32))
+    assert (out[:, :-40] == 0).all()
+    out = prm.int8_matmul(q, s, a, sa, dtype=t)
+    assert torch.equal(out[-40:], prm.int8_matmul(q[-40:].clone(), s[-40:].clone(), a, sa, dtype=t))
+    del q, s, out
+    qt, st = prm.quantize_rows(x, transpose=True)
+    want, sw = eight(end.double().t())
+    assert torch.equal(qt[-1].cpu().double()[-40:], want[-1]) and torch.equal(qt[:, -40:].cpu().double(), want)
+    check_scale(st, sw)
+
+
+def test_layer_of_many_tokens():
+    # more tokens than one piece of the weight's gradient holds
+    t, m, n, k = torch.bfloat16, 140000, 24, 40
+    x, w, gy = rand((m, k), t, 154).cuda().requires_grad_(), rand((n, k), t, 155).cuda().requires_grad_(), rand((m, n), t, 156).cuda()
+    y = prm.int8_linear(x, w)
+    gx, gw = torch.autograd.grad(y, (x, w), gy)
+    (gq, gs), (xq, xs) = (eight(v.detach().cpu().double().t()) for v in (gy, x))
+    want = product64(gq, gs, xq, xs)
+    check(gw, want, 8 * U * want.abs() + half(t) * want.abs() * (1 + 1e-3) + low(t))
+    assert torch.equal(y[-100:], prm.int8_linear(x[-100:].detach(), w.detach()))
+    assert torch.equal(gx[-100:], prm.int8_matmul(*prm.quantize_rows(gy[-100:]), *prm.quantize_rows(w.detach(), transpose=True), dtype=t))
+
+
 def test_product_leaves_what_is_around():
     m, n, k = 70, 35, 50
     a, b, sa, sb = int8s((m, k), 15), int8s((n, k), 16), scales(m, 17), scales(n, 18)
@@ -360,7 +418,7 @@ def test_refusals():
            lambda: prm.quantize_rows(a), lambda: prm.quantize_rows(x[:, :0]),
            lambda: prm.rms_norm(x, x[0].float()), lambda: prm.rms_norm(x, x[0, :8]), lambda: prm.rms_norm(x, residual=x[:2]),
            lambda: prm.rms_norm(x, residual=x.float()), lambda: prm.rms_norm(x.clone().requires_grad_(), quantize=True),
-           lambda: prm.int8_linear(x, x[:, :8]), lambda: prm.int8_linear(x, x.float()), lambda: prm.int8_linear(x, x, x[0])]
+           lambda: prm.int8_linear(x, x[:, :8]), lambda: prm.int8_linear(x, x.float()), lambda: prm.int8_linear(x, x, x[0]), lambda: prm.int8_linear(x, x[:0])]
     for i, f in enumerate(bad):
         with pytest.raises(ValueError):
             f()

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import paper_2608_20818_amd as prm  # noqa: E402
 
 FAKE = 1 << 20  # never dereferenced: the arguments are refused first
@@ -53,7 +54,9 @@ def test_unknown_type(name):
     ("prm_quantize_cols", dict(rows=0)), ("prm_quantize_cols", dict(rows=(1 << 22) + 1, ldq=1 << 30)),
     ("prm_quantize_cols", dict(ldq=3)), ("prm_quantize_cols", dict(ldx=7)), ("prm_quantize_cols", dict(nws=8)),
     ("prm_quantize_cols", dict(ws=None)), ("prm_quantize_cols", dict(x=None)),
-    ("prm_int8_matmul", dict(k=0)), ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072)),
+    ("prm_int8_matmul", dict(k=0)), ("prm_int8_matmul", dict(k=(1 << 20) + 1, lda=1 << 21, ldb=1 << 21)),
+    ("prm_int8_matmul", dict(k=131072, lda=131073, ldb=131072)), ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072)),
+    ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072, ws=FAKE, nws=255)),
     ("prm_int8_matmul", dict(m=-1)), ("prm_int8_matmul", dict(n=(1 << 24) + 1, ldo=1 << 30)),
     ("prm_int8_matmul", dict(lda=7)), ("prm_int8_matmul", dict(ldb=7)), ("prm_int8_matmul", dict(ldo=5)),
     ("prm_int8_matmul", dict(a=None)), ("prm_int8_matmul", dict(sb=None)), ("prm_int8_matmul", dict(out=None)),
@@ -63,10 +66,10 @@ def test_unknown_type(name):
     ("prm_rms_norm", dict(y=None)), ("prm_rms_norm", dict(q=FAKE, ldq=8)), ("prm_rms_norm", dict(y=None, q=FAKE, ldq=8)),
     ("prm_rms_norm", dict(y=None, q=FAKE, ldq=7, scale=FAKE)), ("prm_rms_norm", dict(ldy=7)), ("prm_rms_norm", dict(cols=0)),
     ("prm_rms_norm", dict(x=None)),
-    ("prm_int8_linear", dict(m=-1)), ("prm_int8_linear", dict(n=0)), ("prm_int8_linear", dict(k=131072, ldx=131072, ldw=131072)),
-    ("prm_int8_linear", dict(m=131072)), ("prm_int8_linear", dict(ldx=7)), ("prm_int8_linear", dict(ldw=7)), ("prm_int8_linear", dict(ldy=5)),
+    ("prm_int8_linear", dict(m=-1)), ("prm_int8_linear", dict(n=0)), ("prm_int8_linear", dict(k=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21)),
+    ("prm_int8_linear", dict(m=(1 << 20) + 1)), ("prm_int8_linear", dict(ldx=7)), ("prm_int8_linear", dict(ldw=7)), ("prm_int8_linear", dict(ldy=5)),
     ("prm_int8_linear", dict(nws=64)), ("prm_int8_linear", dict(ws=None)), ("prm_int8_linear", dict(w=None)),
-    ("prm_int8_linear_backward", dict(m=0)), ("prm_int8_linear_backward", dict(n=131072, ldgy=131072)),
+    ("prm_int8_linear_backward", dict(m=0)), ("prm_int8_linear_backward", dict(n=(1 << 20) + 1, ldgy=1 << 21)),
     ("prm_int8_linear_backward", dict(ldgy=5)), ("prm_int8_linear_backward", dict(ldx=7)), ("prm_int8_linear_backward", dict(ldw=7)),
     ("prm_int8_linear_backward", dict(lddx=7)), ("prm_int8_linear_backward", dict(lddw=7)), ("prm_int8_linear_backward", dict(nws=64)),
     ("prm_int8_linear_backward", dict(x=None)), ("prm_int8_linear_backward", dict(w=None)), ("prm_int8_linear_backward", dict(gy=None)),
@@ -109,7 +112,7 @@ def test_workspace_sizes():
         assert f(8192, 4096) % 4 == 0
     assert L.prm_quantize_cols_workspace((1 << 22) + 1, 8) == 0
     for f in (L.prm_int8_linear_workspace, L.prm_int8_linear_backward_workspace):
-        assert f(0, 8, 8) == f(8, 0, 8) == f(8, 8, 0) == f(131072, 8, 8) == 0
+        assert f(0, 8, 8) == f(8, 0, 8) == f(8, 8, 0) == f((1 << 20) + 1, 8, 8) == 0
         assert f(100, 60, 30) >= 100 * 30 + 60 * 30
 
 
@@ -134,6 +137,21 @@ def test_16_bit_values_round_right_without_a_check():
                 k = num // den
                 rest = 2 * (num - k * den)
                 assert np.array_equal(n, k + ((rest > den) | ((rest == den) & (k % 2 == 1)))), (bits, T, j)
+
+
+def test_direct_loads_leave_m0_to_the_compiler(tmp_path):
+    # the products' loads into shared memory write M0 in inline assembly, a register that the
+    # compiler reserves: sound while it reads M0 nowhere itself
+    import subprocess
+
+    from paper_2608_20818_amd import build as b
+    from test_abi import _m0_check
+    out = tmp_path / "ops.s"
+    r = subprocess.run([b.hipcc(), *[f for f in b.FLAGS if f != "-fPIC"], "--cuda-device-only", "-S", os.path.join(b.CSRC, "ops_matmul.hip"),
+                        "-o", str(out)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    readers, asm_dma, bad = _m0_check(out.read_text())
+    assert asm_dma > 0 and readers == 0 and not bad
 
 
 def test_the_step_takes_no_fp16():
