@@ -358,14 +358,15 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
 /* out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] b[j][k] + bias[j], for a
  * (m x k: tokens), b (n x k: output channels, as a linear layer's weight is kept)
  * and out (m x n, type dtype).  The sum is exact (whole numbers), the rest fp32, rounded
- * once.  1 <= k <= 2^20; over 131071, where 128 * 128 k passes 32 bits, the operands' rows
- * have to start on 16-byte boundaries and the workspace has to be there (PRM_EINVAL).
- * bias: n values of type dtype, or NULL.  0 <= m, n <= 2^24.  Operands whose rows start on 16-byte
- * boundaries (a and b, lda and ldb) take faster loads.  `workspace`:
- * prm_int8_matmul_workspace(m, n, k) bytes (0 for most sizes), 16-byte aligned, used by
- * this call only; a product with few outputs and a long sum is split there.  With less,
- * or NULL, one of k <= 131071 is not split: the same result, later. */
-uint64_t prm_int8_matmul_workspace(int64_t m, int64_t n, int64_t k);
+ * once.  1 <= k <= 2^20, 0 <= m, n <= 2^24.  bias: n values of type dtype, or NULL.
+ * `workspace`: prm_int8_matmul_workspace(the same operands and sizes) bytes, 16-byte
+ * aligned, used by this call only: a product with few outputs and a long sum is split
+ * there, and operands whose rows do not start on 16-byte boundaries may be laid out
+ * there anew.  0 bytes for most products of aligned rows.  With less, or NULL, the same
+ * result takes longer; but sums over more than 131071, which pass 32 bits, need it
+ * (PRM_EINVAL). */
+uint64_t prm_int8_matmul_workspace(const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, int64_t m, int64_t n,
+                                   int64_t k);
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
                     const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo,
                     int64_t m, int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes,

@@ -127,7 +127,7 @@ def load() -> ctypes.CDLL:
     L.prm_quantize_cols_workspace.argtypes = [i64, i64]
     L.prm_quantize_cols_workspace.restype = u64
     L.prm_quantize_cols.argtypes = [P, i32, i64, i64, i64, P, i64, P, P, P, u64, P]
-    L.prm_int8_matmul_workspace.argtypes = [i64, i64, i64]
+    L.prm_int8_matmul_workspace.argtypes = [P, i64, P, i64, i64, i64, i64]
     L.prm_int8_matmul_workspace.restype = u64
     L.prm_int8_matmul.argtypes = [P, i64, P, P, i64, P, P, i32, P, i64, i64, i64, i64, P, u64, P]
     L.prm_rms_norm.argtypes = [P, i64, P, i64, P, i32, i64, i64, f32, P, i64, P, i64, P, i64, P, P]

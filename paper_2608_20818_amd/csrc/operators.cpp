@@ -176,7 +176,8 @@ PyObject* int8_matmul(PyObject*, PyObject* const* args, Py_ssize_t n) {
         !vector_of(*sb, *a, at::kFloat, rb.rows) || (bias && !vector_of(*bias, *a, type_of(code), rb.rows)))
       Py_RETURN_NONE;
     at::Tensor out = with_last(lead_of(*a), rb.rows, *a, type_of(code));
-    const uint64_t need = prm_int8_matmul_workspace(ra.rows, rb.rows, ra.cols);
+    const uint64_t need = prm_int8_matmul_workspace((const int8_t*)a->const_data_ptr(), ra.ld, (const int8_t*)b->const_data_ptr(), rb.ld,
+                                                    ra.rows, rb.rows, ra.cols);
     at::Tensor ws = bytes(need, *a);
     check(prm_int8_matmul((const int8_t*)a->const_data_ptr(), ra.ld, (const float*)sa->const_data_ptr(), (const int8_t*)b->const_data_ptr(),
                           rb.ld, (const float*)sb->const_data_ptr(), data(bias), (int32_t)code, out.data_ptr(), rb.rows, ra.rows, rb.rows,

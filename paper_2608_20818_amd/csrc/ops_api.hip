@@ -142,12 +142,12 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   return launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream));
 }
 
-// prm_int8_matmul; `kind` and `splits`: a ProductPlan, or 0 for the rule's (tests hold
+// prm_int8_matmul; `kind`, `splits`, `pack`: a ProductPlan, or 0 for the rule's (tests hold
 // every kernel to the sizes that it takes).
 int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
                              const float* b_scale, const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m,
                              int64_t n, int64_t k, void* workspace, uint64_t workspace_bytes, void* hip_stream,
-                             int32_t kind, int32_t splits) {
+                             int32_t kind, int32_t splits, int32_t pack) {
   static const char* const call = "prm_int8_matmul";
   TRY(check_type(dtype));
   if (m < 0 || n < 0 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK)
@@ -158,38 +158,42 @@ int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale,
   TRY(check_ld(call, "ldo", ldo, n));
   if (m == 0 || n == 0) return PRM_OK;
   ProductArgs p = {a, b, a_scale, b_scale, bias, out, m, n, k, lda, ldb, ldo, (int32_t*)workspace};
-  ProductPlan plan = {(ProductKind)kind, splits};
+  ProductPlan plan = {(ProductKind)kind, splits, pack};
   if (kind == 0) {
-    plan = product_plan(p);
+    // without the room that the fastest plan needs, the same sums by another
+    plan = product_plan(p, true);
+    if (!workspace || workspace_bytes < product_workspace(p, plan)) plan = product_plan(p, false);
     if (!product_takes(p, plan))
-      return fail(PRM_EINVAL, "%s: sums over more than %lld need rows on 16-byte boundaries", call, (long long)kMaxPieceK);
-    // without the room that a split needs, the same sums in one piece
-    if (k <= kMaxPieceK && (!workspace || workspace_bytes < product_workspace(m, n, plan.splits))) plan.splits = 1;
+      return fail(PRM_EINVAL, "%s: sums over more than %lld need their workspace", call, (long long)kMaxPieceK);
   } else if (kind < 0 || kind >= PRODUCT_KINDS || !product_takes(p, plan)) {
-    return fail(PRM_EINVAL, "%s: kernel %d does not take this product in %d", call, kind, splits);
+    return fail(PRM_EINVAL, "%s: kernel %d does not take this product in %d, %d", call, kind, splits, pack);
   }
-  if (plan.splits > 1) TRY(check_workspace(call, workspace, workspace_bytes, product_workspace(m, n, plan.splits)));
+  const uint64_t need = product_workspace(p, plan);
+  if (need) TRY(check_workspace(call, workspace, workspace_bytes, need));
   TRY(check_buffers(call, {{a, "a", 1}, {a_scale, "a_scale", 4}, {b, "b", 1}, {b_scale, "b_scale", 4},
                            optional(bias, "bias", size_of(dtype)), {out, "out", size_of(dtype)},
-                           optional(plan.splits > 1 ? workspace : nullptr, "workspace", 16)}));
+                           optional(need ? workspace : nullptr, "workspace", 16)}));
   return launched(call, launch_int8_matmul((OpType)dtype, p, plan, (hipStream_t)hip_stream));
 }
 
-uint64_t prm_int8_matmul_workspace(int64_t m, int64_t n, int64_t k) {
-  if (m < 1 || n < 1 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK) return 0;
+uint64_t prm_int8_matmul_workspace(const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, int64_t m, int64_t n, int64_t k) {
+  if (m < 1 || n < 1 || m > kMaxCols || n > kMaxCols || k < 1 || k > kMaxProductK || lda < k || ldb < k) return 0;
   ProductArgs p = {};
+  p.a = a;
+  p.b = b;
+  p.lda = lda;
+  p.ldb = ldb;
   p.m = m;
   p.n = n;
   p.k = k;
-  p.lda = p.ldb = (k + 15) / 16 * 16;
-  return product_workspace(m, n, product_plan(p).splits);
+  return product_workspace(p, product_plan(p, true));
 }
 
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
                     const void* bias, int32_t dtype, void* out, int64_t ldo, int64_t m, int64_t n, int64_t k,
                     void* workspace, uint64_t workspace_bytes, void* hip_stream) {
   return prm_internal_int8_matmul(a, lda, a_scale, b, ldb, b_scale, bias, dtype, out, ldo, m, n, k, workspace,
-                                  workspace_bytes, hip_stream, 0, 0);
+                                  workspace_bytes, hip_stream, 0, 0, 0);
 }
 
 // The layer's operands in 8 bits, their scales and the statistics' partial sums, one after
@@ -222,6 +226,11 @@ static QuantArgs quantiser(Layout& l, const void* x, int64_t rows, int64_t cols,
   }
   return a;
 }
+// The workspace of the product of two such operands: their rows start on 16-byte boundaries.
+static uint64_t part_bytes(int64_t m, int64_t n, int64_t k) {
+  const int64_t ld = (k + 15) / 16 * 16;
+  return prm_int8_matmul_workspace(nullptr, ld, nullptr, ld, m, n, k);
+}
 // p^T q of two quantised operands (k: the length of their rows), split where the rule does
 static ProductArgs product_of(const QuantArgs& p, const QuantArgs& q, int64_t m, int64_t n, int64_t k, const void* bias, void* out,
                               int64_t ldo, void* part) {
@@ -236,7 +245,7 @@ struct LinearForward {
     Layout l{base};
     x = quantiser(l, xp, m, k, ldx, false, nullptr);
     w = quantiser(l, wp, n, k, ldw, false, nullptr);
-    part = l.take(prm_int8_matmul_workspace(m, n, k));
+    part = l.take(part_bytes(m, n, k));
     bytes = l.used;
   }
 };
@@ -251,7 +260,7 @@ struct LinearBackward {
     wt = quantiser(l, wp, n, k, ldw, true, nullptr);
     gt = quantiser(l, gp, m, n, ldg, true, db);
     xt = quantiser(l, xp, m, k, ldx, true, nullptr);
-    const uint64_t a = prm_int8_matmul_workspace(m, k, n), b = prm_int8_matmul_workspace(n, k, m);
+    const uint64_t a = part_bytes(m, k, n), b = part_bytes(n, k, m);
     part = l.take(a > b ? a : b);  // the products run one after the other
     bytes = l.used;
   }
@@ -290,7 +299,7 @@ int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
   jobs.n = 2;
   TRY(launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream)));
   const ProductArgs p = product_of(f.x, f.w, m, n, k, bias, y, ldy, f.part);
-  return launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), (hipStream_t)hip_stream));
+  return launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), (hipStream_t)hip_stream));
 }
 
 uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
@@ -334,11 +343,11 @@ int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_
   TRY(launched(call, launch_quantize((OpType)dtype, jobs, s)));
   if (dx) {
     const ProductArgs p = product_of(f.g, f.wt, m, k, n, nullptr, dx, lddx, f.part);
-    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), s)));
+    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), s)));
   }
   if (dw) {
     const ProductArgs p = product_of(f.gt, f.xt, n, k, m, nullptr, dw, lddw, f.part);
-    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p), s)));
+    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), s)));
   }
   return PRM_OK;
 }

@@ -80,7 +80,8 @@ struct ProductArgs {
   int32_t* part;     // the splits' sums, or nullptr
 };
 // The kernels, by tile; ANY: rows that start on any byte.  The piped ones (64, 128) can
-// split k over blocks, whose sums meet in `part` (product_workspace bytes).
+// split k over blocks, whose sums meet in `part` (product_workspace bytes), and, as 256, take
+// operands that were laid out anew.
 enum ProductKind : int32_t {
   PRODUCT_FEW = 1, PRODUCT_ANY64, PRODUCT_ANY128, PRODUCT_64, PRODUCT_128, PRODUCT_128_PAIRED, PRODUCT_256,
   PRODUCT_KINDS
@@ -88,10 +89,18 @@ enum ProductKind : int32_t {
 struct ProductPlan {
   ProductKind kind;
   int32_t splits;
+  int32_t pack;  // 1: a, 2: b laid out anew, in `part` before the splits' sums
 };
 bool product_takes(const ProductArgs& p, const ProductPlan& plan);
-ProductPlan product_plan(const ProductArgs& p);  // the rule
-uint64_t product_workspace(int64_t m, int64_t n, int32_t splits);
+ProductPlan product_plan(const ProductArgs& p, bool workspace);  // the rule, with or without a workspace
+uint64_t product_workspace(const ProductArgs& p, const ProductPlan& plan);
+// pack_kernel: rows of k bytes, ld apart, to rows of kp
+struct PackArgs {
+  const int8_t* src[2];
+  int8_t* dst[2];
+  int64_t rows[2], ld[2];
+  int64_t k, kp;
+};
 hipError_t launch_int8_matmul(OpType t, const ProductArgs& p, const ProductPlan& plan, hipStream_t s);
 // 128 * 128 k stays below 2^31 in one piece; longer sums are split and joined in 64 bits
 constexpr int64_t kMaxPieceK = 131071, kMaxProductK = 1 << 20;

@@ -608,6 +608,21 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p, int splits) {
   store_row8<E>((typename E::S*)p.out + row * p.ldo, c, p.n, E::pack(v));
 }
 
+// Operands whose rows start on any byte, laid out for the direct loads: rows of kp (a
+// multiple of 128) bytes, zeros behind the end.  16 bytes a thread.
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs g) {
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int which = i >= g.rows[0] * (g.kp / 16);
+  if (which) i -= g.rows[0] * (g.kp / 16);
+  const int64_t per = g.kp / 16, row = i / per, k = 16 * (i - row * per);
+  if (row >= g.rows[which]) return;
+  const int8_t* src = g.src[which] + row * g.ld[which];
+  u32x4_t v = {0u, 0u, 0u, 0u};
+  if (k + 16 <= g.k) v = load16(src + k);
+  else if (k < g.k) v = load_k16(src, k, g.k);
+  *(PRM_GLOBAL u32x4_t*)(g.dst[which] + row * g.kp + k) = v;
+}
+
 template <class E, int BM, int NBUF>
 void launch_piped(const ProductArgs& p, int splits, hipStream_t s) {
   const int tm = (int)((p.m + BM - 1) / BM), tn = (int)((p.n + BM - 1) / BM);
@@ -620,7 +635,29 @@ void launch_piped(const ProductArgs& p, int splits, hipStream_t s) {
 }
 
 template <class E>
-hipError_t launch(const ProductArgs& p, const ProductPlan& plan, hipStream_t s) {
+hipError_t launch(ProductArgs p, const ProductPlan& plan, hipStream_t s) {
+  if (plan.pack) {
+    PackArgs g = {};
+    g.k = p.k;
+    g.kp = (p.k + 127) / 128 * 128;
+    int8_t* at = (int8_t*)p.part;
+    const auto lay = [&](const int8_t*& operand, int64_t& ld, int64_t rows, int which) {
+      g.src[which] = operand;
+      g.ld[which] = ld;
+      g.dst[which] = at;
+      g.rows[which] = rows;
+      operand = at;
+      ld = g.kp;
+      at += rows * g.kp;
+    };
+    if (plan.pack & 1) lay(p.a, p.lda, p.m, 0);
+    if (plan.pack & 2) lay(p.b, p.ldb, p.n, 1);
+    const int64_t pieces = (g.rows[0] + g.rows[1]) * (g.kp / 16);
+    if (pieces >= kMaxTiles * 256) return hipErrorInvalidValue;
+    pack_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, s>>>(g);
+    if (plan.pack == 3) p.k = g.kp;  // zeros behind both ends: no end within a piece
+    p.part = (int32_t*)at;
+  }
   const int64_t b = plan.kind == PRODUCT_256 ? 256 : plan.kind == PRODUCT_ANY64 ? 64 : 128;
   const int64_t tm = (p.m + b - 1) / b, tn = (p.n + b - 1) / b;
   if (tm * tn >= kMaxTiles) return hipErrorInvalidValue;
@@ -639,22 +676,27 @@ hipError_t launch(const ProductArgs& p, const ProductPlan& plan, hipStream_t s) 
 
 }  // namespace
 
+// the direct loads' 16-byte granule, and 32-bit offsets within a tile
+static bool direct(const int8_t* p, int64_t ld) { return ld % 16 == 0 && (uintptr_t)p % 16 == 0 && ld < (1 << 23); }
+
 bool product_takes(const ProductArgs& p, const ProductPlan& plan) {
   const ProductKind kind = plan.kind;
   const int64_t pieces = p.k / 128;
+  if (plan.pack && (kind < PRODUCT_64 || plan.pack > 3)) return false;
   if (plan.splits == 1 ? p.k > kMaxPieceK : plan.splits > 1 && ((pieces + plan.splits - 1) / plan.splits + 1) * 128 > kMaxPieceK)
     return false;  // a piece's sum has to fit 32 bits
   if (plan.splits != 1 && (kind < PRODUCT_64 || kind == PRODUCT_256 || plan.splits < 1 || plan.splits > pieces || plan.splits > 64))
     return false;
   if (kind == PRODUCT_FEW) return p.m <= 16;
   if (kind == PRODUCT_ANY64 || kind == PRODUCT_ANY128) return true;
-  // direct loads need their 16-byte granule, and 32-bit offsets within a tile
-  return p.lda % 16 == 0 && p.ldb % 16 == 0 && (uintptr_t)p.a % 16 == 0 && (uintptr_t)p.b % 16 == 0 && p.lda < (1 << 23) &&
-         p.ldb < (1 << 23);
+  // operands that are laid out anew, or that the direct loads take as they are
+  return ((plan.pack & 1) || direct(p.a, p.lda)) && ((plan.pack & 2) || direct(p.b, p.ldb));
 }
 
-uint64_t product_workspace(int64_t m, int64_t n, int32_t splits) {
-  return splits > 1 ? (uint64_t)splits * (uint64_t)m * (uint64_t)((n + 7) / 8 * 8) * 4 : 0;
+uint64_t product_workspace(const ProductArgs& p, const ProductPlan& plan) {
+  const uint64_t kp = (uint64_t)((p.k + 127) / 128 * 128);
+  return (plan.pack & 1 ? (uint64_t)p.m * kp : 0) + (plan.pack & 2 ? (uint64_t)p.n * kp : 0) +
+         (plan.splits > 1 ? (uint64_t)plan.splits * (uint64_t)p.m * (uint64_t)((p.n + 7) / 8 * 8) * 4 : 0);
 }
 
 // The least of the kernels' estimated times, in microseconds: rounds of tiles over the 256
@@ -671,35 +713,39 @@ uint64_t product_workspace(int64_t m, int64_t n, int32_t splits) {
 // Splitting k costs a second launch and the sums' way through memory at about 2 TB/s:
 // 64 x 4096 x 16384 takes 37.7 us in one piece (64), 21.6 in 4; 1024 x 1024 x 65536
 // 147 (64) and 99 (128 in 4); 64 x 4096 x 4096 9.4, and 10.7 in 2.
-ProductPlan product_plan(const ProductArgs& p) {
-  if (p.m <= 8 && p.k <= kMaxPieceK) return {PRODUCT_FEW, 1};
+// Rows that start anywhere are read as they are (ANY64, ANY128), or laid out anew first (a
+// launch, and both ways through memory at about 4 TB/s): 4096 x 4096 x 4097 takes 244 us
+// on ANY64, 177 on ANY128, and 81 laid out for 256; 64 x 6144 x 2047 12 us on ANY64, 17 laid
+// out.  Few tokens' kernel reads any rows at one speed.
+ProductPlan product_plan(const ProductArgs& p, bool workspace) {
+  if (p.m <= 8 && p.k <= kMaxPieceK) return {PRODUCT_FEW, 1, 0};
+  const int pack = (direct(p.a, p.lda) ? 0 : 1) | (direct(p.b, p.ldb) ? 0 : 2);
+  if (pack && p.m <= 16 && p.k <= kMaxPieceK) return {PRODUCT_FEW, 1, 0};
   const auto tiles = [&](int64_t b) { return (double)((p.m + b - 1) / b) * (double)((p.n + b - 1) / b); };
-  ProductArgs q = p;
-  q.k = 128;  // the rows' alignment alone
-  if (!product_takes(q, {PRODUCT_256, 1})) {
-    if (p.m <= 16) return {PRODUCT_FEW, 1};
-    // rows that start anywhere: 4096 x 4096 x 4097 takes 229 us on 64, 146 on 128;
-    // 777 x 1011 x 1357 (56 tiles of 128) 11 and 27
-    return {tiles(128) >= 256 ? PRODUCT_ANY128 : PRODUCT_ANY64, 1};
-  }
   const double stages = (double)((p.k + 127) / 128);
   const auto rounds = [](double t, double at_once) { return std::ceil(t / at_once); };
   const auto fill = [](double t) { return t < 256 ? t / 256 : 1.0; };
   double best = 1e30;
-  ProductPlan plan = {PRODUCT_64, 64};
-  const auto take = [&](ProductKind kind, int splits, double t) {
-    if (t < best && product_takes(p, {kind, splits})) {
+  ProductPlan plan = {PRODUCT_64, 64, pack};
+  const auto take = [&](ProductKind kind, int splits, int packed, double t) {
+    const ProductPlan q = {kind, splits, packed};
+    if (t < best && (workspace || !product_workspace(p, q)) && product_takes(p, q)) {
       best = t;
-      plan = {kind, splits};
+      plan = q;
     }
   };
-  take(PRODUCT_256, 1, 14 + rounds(tiles(256), 256) * (stages * (0.95 + 0.6 * fill(tiles(256))) + 9) - 9);
-  take(PRODUCT_128_PAIRED, 1, 4 + rounds(tiles(128), 512) * (stages * 1.15 + 4));
+  if (pack) {
+    take(PRODUCT_ANY64, 1, 0, 3.5 + rounds(tiles(64), 256) * stages * (tiles(64) <= 256 ? 0.65 : 0.43));
+    take(PRODUCT_ANY128, 1, 0, 4.5 + rounds(tiles(128), 256) * (stages * 1.1 + 2));
+  }
+  const double laid = pack ? 3.5 + ((pack & 1 ? (double)p.m : 0) + (pack & 2 ? (double)p.n : 0)) * stages * 128 * 2 / 4e6 : 0;
+  take(PRODUCT_256, 1, pack, laid + 14 + rounds(tiles(256), 256) * (stages * (0.95 + 0.6 * fill(tiles(256))) + 9) - 9);
+  take(PRODUCT_128_PAIRED, 1, pack, laid + 4 + rounds(tiles(128), 512) * (stages * 1.15 + 4));
   for (int s = 1; s == 1 || (s <= 16 && stages >= 8 * s); s *= 2) {
     const double n = std::ceil(stages / s);
-    const double join = s == 1 ? 0 : 3.5 + s * (double)p.m * (double)p.n * 4 / 2e6;
-    take(PRODUCT_128, s, 4.5 + rounds(s * tiles(128), 256) * (n * (0.45 + 0.15 * fill(s * tiles(128))) + 4) - 4 + join);
-    take(PRODUCT_64, s, 3.2 + rounds(s * tiles(64), 256) * (n * (0.2 + 0.06 * fill(s * tiles(64) / 4)) + 0.6) - 0.6 + join);
+    const double join = laid + (s == 1 ? 0 : 3.5 + s * (double)p.m * (double)p.n * 4 / 2e6);
+    take(PRODUCT_128, s, pack, 4.5 + rounds(s * tiles(128), 256) * (n * (0.45 + 0.15 * fill(s * tiles(128))) + 4) - 4 + join);
+    take(PRODUCT_64, s, pack, 3.2 + rounds(s * tiles(64), 256) * (n * (0.2 + 0.06 * fill(s * tiles(64) / 4)) + 0.6) - 0.6 + join);
   }
   return plan;
 }

@@ -147,9 +147,8 @@ def _quantize_cols(x, with_sum):
 def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     """``a_scale a (b_scale b)^T + bias``: the product of 8-bit operands, ``a``
     ``[..., k]`` with a scale for each row (token) and ``b`` ``[n, k]`` with one for each
-    row (output channel, as a linear layer's weight is kept); ``bias`` ``[n]`` and the
-    result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 2^20; over 131071, of
-    rows on 16-byte boundaries, as ``quantize_rows`` gives them) is exact;
+    row (output channel, as a linear layer's weight is kept; rows on 16-byte boundaries, as
+    ``quantize_rows`` gives them, are the fast ones); ``bias`` ``[n]`` and the result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 2^20) is exact;
     scales and bias are applied in fp32 and the result rounded once.  Not
     differentiable (``int8_linear`` is)."""
     r = _native.int8_matmul(a, a_scale, b, b_scale, bias, _CODE.get(dtype, -1))
@@ -179,7 +178,7 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
         sa, sb = a_scale.contiguous(), b_scale.contiguous()
         bv = None if bias is None else _vector(bias.detach())
         L = load()
-        need = L.prm_int8_matmul_workspace(rows, n, k)
+        need = L.prm_int8_matmul_workspace(m.data_ptr(), lda, bm.data_ptr(), ldb, rows, n, k)
         ws = torch.empty(need, dtype=torch.uint8, device=a.device) if need else None
         _check(L.prm_int8_matmul(m.data_ptr(), lda, sa.data_ptr(), bm.data_ptr(), ldb, sb.data_ptr(),
                                  None if bv is None else bv.data_ptr(), _CODE[dtype], out.data_ptr(), max(n, 1),

@@ -239,7 +239,8 @@ def check_product(got, a, sa, b, sb, bias, t):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 64), (1, 1000, 515), (3, 17, 33), (7, 130, 256), (16, 64, 129), (17, 100, 1000), (31, 33, 31), (32, 48, 4096),
             (33, 15, 700), (64, 200, 640), (65, 64, 128), (65, 63, 127), (128, 128, 128), (129, 130, 257), (200, 1, 100), (255, 257, 1024),
-            (300, 700, 391), (2049, 2047, 160), (2305, 2304, 384), (512, 4096, 144)]
+            (300, 700, 391), (2049, 2047, 160), (2305, 2304, 384), (512, 4096, 144),
+            (1500, 1501, 2049), (40, 5000, 9001)]
 
 
 @pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
@@ -265,8 +266,10 @@ def test_product_strides(m):
 
 
 # kernels by number (1: few tokens, 2 and 3: rows on any byte, tiles of 64 and 128, 4 to 6: 64,
-# 128, 128 with two buffers, 7: 256), and in how many pieces k is split
-KERNELS = [(1, 1), (2, 1), (3, 1), (4, 1), (5, 1), (6, 1), (7, 1), (4, 2), (4, 7), (5, 3), (6, 2)]
+# 128, 128 with two buffers, 7: 256), in how many pieces k is split, and which operands are
+# laid out anew (1: a, 2: b)
+KERNELS = [(1, 1, 0), (2, 1, 0), (3, 1, 0), (4, 1, 0), (5, 1, 0), (6, 1, 0), (7, 1, 0), (4, 2, 0), (4, 7, 0), (5, 3, 0), (6, 2, 0), (4, 1, 3), (4, 3, 3),
+           (5, 1, 1), (5, 2, 2), (6, 1, 3), (7, 1, 1), (7, 1, 2), (7, 1, 3)]
 SIZES = [(1, 1, 1), (3, 65, 515), (16, 100, 3000), (65, 64, 16), (70, 50, 128), (129, 257, 400), (300, 300, 1000), (257, 511, 1072), (513, 130, 1152),
          (64, 70, 8192), (520, 900, 2053)]
 
@@ -274,21 +277,23 @@ SIZES = [(1, 1, 1), (3, 65, 515), (16, 100, 3000), (65, 64, 16), (70, 50, 128), 
 @pytest.mark.parametrize("kernel", KERNELS, ids=str)
 def test_every_kernel(kernel):
     # every kernel at every size that it takes, whatever the rule would choose
-    kind, splits = kernel
+    kind, splits, pack = kernel
     P, i64, i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
     f = prm.load().prm_internal_int8_matmul
-    f.argtypes = [P, i64, P, P, i64, P, P, i32, P, i64, i64, i64, i64, P, ctypes.c_uint64, P, i32, i32]
+    f.argtypes = [P, i64, P, P, i64, P, P, i32, P, i64, i64, i64, i64, P, ctypes.c_uint64, P, i32, i32, i32]
     ran = 0
     for m, n, k in SIZES:
-        ld = (k + 15) // 16 * 16 if kind > 3 else k + k % 2
+        even, any_ = (k + 15) // 16 * 16, k + k % 2
+        lda = any_ if kind <= 3 or pack & 1 else even
+        ldb = any_ if kind <= 3 or pack & 2 else even
         a, b, sa, sb, t = int8s((m, k), 22), int8s((n, k), 23), scales(m, 24), scales(n, 25), torch.float32
-        ag, bg = on_gpu(a, ld, 0), on_gpu(b, ld, 0)
+        ag, bg = on_gpu(a, lda, pack & 1), on_gpu(b, ldb, 3 * (pack & 2))
         bias = rand((n,), t, 26)
-        ws = torch.empty(splits * m * (n + 7) * 4, dtype=torch.uint8, device="cuda")
+        ws = torch.empty(splits * m * (n + 7) * 4 + (m + n) * (k + 127), dtype=torch.uint8, device="cuda")
         out = torch.full((m + 1, n + 3), 7.0, device="cuda")
         sag, sbg, biasg = sa.cuda(), sb.cuda(), bias.cuda()
-        rc = f(ag.data_ptr(), ld, sag.data_ptr(), bg.data_ptr(), ld, sbg.data_ptr(), biasg.data_ptr(), prm.F32, out.data_ptr(), n + 3, m, n, k,
-               ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream, kind, splits)
+        rc = f(ag.data_ptr(), lda, sag.data_ptr(), bg.data_ptr(), ldb, sbg.data_ptr(), biasg.data_ptr(), prm.F32, out.data_ptr(), n + 3, m, n, k,
+               ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream, kind, splits, pack)
         if rc == prm.PRM_EINVAL and (kind == 1 and m > 16 or splits > k // 128):
             continue
         assert rc == prm.PRM_OK, prm.load().prm_last_error()
@@ -303,7 +308,7 @@ def test_product_without_its_workspace():
     m, n, k = 40, 200, 16000
     a, b, sa, sb = int8s((m, k), 27).cuda(), int8s((n, k), 28).cuda(), scales(m, 29).cuda(), scales(n, 30).cuda()
     L = prm.load()
-    assert L.prm_int8_matmul_workspace(m, n, k) > 0 and L.prm_int8_matmul_workspace(4096, 4096, 4096) == 0
+    assert L.prm_int8_matmul_workspace(a.data_ptr(), k, b.data_ptr(), k, m, n, k) > 0
     want = prm.int8_matmul(a, sa, b, sb, dtype=torch.float32)
     got = torch.empty_like(want)
     for ws, need in ((None, 0), (torch.empty(16, dtype=torch.uint8, device="cuda"), 16)):
@@ -337,9 +342,8 @@ def test_product_of_sums_past_32_bits(m, k):
     b.copy_(torch.randint(-128, 128, (n, k), dtype=torch.int8, device="cuda", generator=g))
     got = prm.int8_matmul(a, one[:m], b, one[:n], dtype=torch.float32)
     assert torch.equal(got, (a.double() @ b.double().t()).float())
-    if k % 16:
-        with pytest.raises(prm.PRMError):
-            prm.int8_matmul(a.contiguous(), one[:m], b, one[:n])
+    if k % 16:  # rows on any byte
+        assert torch.equal(got, prm.int8_matmul(a.contiguous(), one[:m], b, one[:n], dtype=torch.float32))
 
 
 def test_offsets_past_32_bits():

@@ -55,7 +55,8 @@ def test_unknown_type(name):
     ("prm_quantize_cols", dict(ldq=3)), ("prm_quantize_cols", dict(ldx=7)), ("prm_quantize_cols", dict(nws=8)),
     ("prm_quantize_cols", dict(ws=None)), ("prm_quantize_cols", dict(x=None)),
     ("prm_int8_matmul", dict(k=0)), ("prm_int8_matmul", dict(k=(1 << 20) + 1, lda=1 << 21, ldb=1 << 21)),
-    ("prm_int8_matmul", dict(k=131072, lda=131073, ldb=131072)), ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072)),
+    ("prm_int8_matmul", dict(k=131072, lda=131073, ldb=131072)),
+    ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072)),
     ("prm_int8_matmul", dict(k=131072, lda=131072, ldb=131072, ws=FAKE, nws=255)),
     ("prm_int8_matmul", dict(m=-1)), ("prm_int8_matmul", dict(n=(1 << 24) + 1, ldo=1 << 30)),
     ("prm_int8_matmul", dict(lda=7)), ("prm_int8_matmul", dict(ldb=7)), ("prm_int8_matmul", dict(ldo=5)),
@@ -111,6 +112,13 @@ def test_workspace_sizes():
         assert f(1, 1) > 0 and f(8192, 4096) >= 4 * 4096
         assert f(8192, 4096) % 4 == 0
     assert L.prm_quantize_cols_workspace((1 << 22) + 1, 8) == 0
+    w = L.prm_int8_matmul_workspace
+    assert w(FAKE, 4096, FAKE, 4096, 4096, 4096, 4096) == 0  # one piece, rows as they are
+    assert w(FAKE, 16000, FAKE, 16000, 40, 200, 16000) >= 2 * 40 * 200 * 4  # split
+    # one operand laid out anew, the other, both
+    assert w(FAKE, 4097, FAKE, 4096, 4096, 8192, 4096) == 4096 * 4096 and w(FAKE, 4096, FAKE + 8, 4096, 4096, 8192, 4096) == 8192 * 4096
+    assert w(FAKE, 4097, FAKE, 4097, 4096, 8192, 4097) == 3 * 4096 * 4224
+    assert w(FAKE, 4096, FAKE, 4096, 0, 8, 4096) == 0 and w(FAKE, 8, FAKE, 16, 8, 8, 16) == 0
     for f in (L.prm_int8_linear_workspace, L.prm_int8_linear_backward_workspace):
         assert f(0, 8, 8) == f(8, 0, 8) == f(8, 8, 0) == f((1 << 20) + 1, 8, 8) == 0
         assert f(100, 60, 30) >= 100 * 30 + 60 * 30
