@@ -68,7 +68,7 @@ int launched(const char* call, hipError_t e) {
   return e == hipSuccess ? PRM_OK : fail(PRM_EHIP, "%s: launch failed: %s", call, hipGetErrorString(e));
 }
 int check_workspace(const char* call, const void* p, uint64_t have, uint64_t need) {
-  if (have < need || !p)
+  if (need && (have < need || !p))
     return fail(PRM_EINVAL, "%s: the workspace has %llu bytes, needs %llu", call, (unsigned long long)(p ? have : 0),
                 (unsigned long long)need);
   return PRM_OK;
@@ -107,7 +107,7 @@ int prm_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
 uint64_t prm_quantize_cols_workspace(int64_t rows, int64_t cols) {
   if (rows < 1 || rows > kMaxColRows || cols < 1 || cols > kMaxCols) return 0;
   int32_t nrb, per;
-  quantize_cols_blocks(rows, cols, &nrb, &per);
+  quantize_cols_blocks(rows, cols, false, &nrb, &per);
   return (uint64_t)nrb * (uint64_t)cols * 8;
 }
 
@@ -132,7 +132,8 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   a.cols = cols;
   a.ldx = ldx;
   a.ldq = ldq;
-  quantize_cols_blocks(rows, cols, &a.nrb, &a.rows_per_block);
+  // sums are added in one order, alone or in the layer's gradients
+  quantize_cols_blocks(rows, cols, !sum, &a.nrb, &a.rows_per_block);
   a.part_max = (uint32_t*)workspace;
   a.part_sum = (float*)workspace + (int64_t)a.nrb * cols;
   QuantJobs jobs = {};
@@ -220,7 +221,7 @@ static QuantArgs quantiser(Layout& l, const void* x, int64_t rows, int64_t cols,
   a.q = (int8_t*)l.take((uint64_t)out_rows * (uint64_t)a.ldq);
   a.scale = (float*)l.take((uint64_t)out_rows * 4);
   if (columns) {
-    quantize_cols_blocks(rows, cols, &a.nrb, &a.rows_per_block);
+    quantize_cols_blocks(rows, cols, false, &a.nrb, &a.rows_per_block);
     a.part_max = (uint32_t*)l.take((uint64_t)a.nrb * (uint64_t)cols * 4);
     a.part_sum = (float*)l.take((uint64_t)a.nrb * (uint64_t)cols * 4);
   }

@@ -85,6 +85,25 @@ struct TF16 {
   __device__ __forceinline__ static void store1(S* p, float v) { *gptr(p) = (uint16_t)down(v); }
 };
 
+// 16-bit elements moved down by n of 8, zeros behind
+__device__ __forceinline__ u32x4e_t moved_down(const u32x4e_t& r, int n) {
+  const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+  const int b = 16 * n;
+  const uint64_t l = b == 0 ? lo : b < 64 ? lo >> b | hi << (64 - b) : hi >> (b - 64);
+  const uint64_t h = b < 64 ? hi >> b : 0;
+  return u32x4e_t{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+__device__ __forceinline__ TF32::Raw moved_down(const TF32::Raw& r, int n) {
+  float v[8];
+  TF32::expand(r, v);
+#pragma unroll
+  for (int step = 1; step < 8; step <<= 1) {
+    const bool on = n & step;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = on ? (k + step < 8 ? v[k + step] : 0.f) : v[k];
+  }
+  return TF32::pack(v);
+}
 // 8 elements of a row at column c < cols: whole, or the row's last ones with zeros behind
 template <class E>
 __device__ __forceinline__ typename E::Raw load_row8(const typename E::S* row, int64_t c, int64_t cols) {
@@ -93,6 +112,16 @@ __device__ __forceinline__ typename E::Raw load_row8(const typename E::S* row, i
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? E::load1(row + c + k) : 0.f;
   return E::pack(v);  // exact: the values are of the type
+}
+// The same in one load: at the row's end its last 8 elements, moved down.  For sweeps that
+// wait for each load (statistics of 1024 x 645: 12 us, with the other 14); it costs
+// registers that the kernels of whole rows need (gradient of 8192 x 4096: 69 us, 55).
+template <class E>
+__device__ __forceinline__ typename E::Raw load_end8(const typename E::S* row, int64_t c, int64_t cols) {
+  if (cols < 8) return load_row8<E>(row, c, cols);
+  const int64_t from = min(c, cols - 8);
+  const typename E::Raw r = E::load8(row + from);
+  return c == from ? r : moved_down(r, (int)(c - from));
 }
 template <class E>
 __device__ __forceinline__ void store_row8(typename E::S* row, int64_t c, int64_t cols, const typename E::Raw& r) {

@@ -38,7 +38,7 @@ struct QuantArgs {
   uint32_t* part_max;
   float* part_sum;
   void* sum;  // column sums in the type of x, or nullptr
-  int32_t nrb, rows_per_block;
+  int32_t nrb, rows_per_block;  // nrb 0: none, the tiles take their columns' statistics
 };
 hipError_t launch_quantize_rows(OpType t, const QuantArgs& a, hipStream_t s);
 // Up to four quantisers of one type, by rows or (`columns`) by columns, in one launch for
@@ -50,8 +50,8 @@ struct QuantJobs {
   int32_t n;
 };
 hipError_t launch_quantize(OpType t, const QuantJobs& jobs, hipStream_t s);
-// row blocks of the columns' statistics
-void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block);
+// row blocks of the columns' statistics; alone: of a launch without other quantisers
+void quantize_cols_blocks(int64_t rows, int64_t cols, bool alone, int32_t* nrb, int32_t* rows_per_block);
 
 struct NormGradArgs {
   const void* gy;

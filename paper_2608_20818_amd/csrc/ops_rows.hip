@@ -484,11 +484,11 @@ __device__ __forceinline__ void col_stats(const QuantArgs& a, int bx, int by, Co
     for (; r + 24 < r1; r += 32) {  // four rows' loads together
       typename E::Raw raw[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) raw[i] = load_row8<E>((const S*)a.x + (r + 8 * i) * a.ldx, c, a.cols);
+      for (int i = 0; i < 4; ++i) raw[i] = load_end8<E>((const S*)a.x + (r + 8 * i) * a.ldx, c, a.cols);
 #pragma unroll
       for (int i = 0; i < 4; ++i) add(raw[i]);
     }
-    for (; r < r1; r += 8) add(load_row8<E>((const S*)a.x + r * a.ldx, c, a.cols));
+    for (; r < r1; r += 8) add(load_end8<E>((const S*)a.x + r * a.ldx, c, a.cols));
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
@@ -519,7 +519,8 @@ struct ColQuantShared {
   float ps[4][64];
   EightOf<E> eights[64];
 };
-template <class E, bool SUM>
+// OWN: a job may have no statistics laid out (its registers cost the others three waves of eight).
+template <class E, bool SUM, bool OWN>
 __device__ __forceinline__ void col_quant(const QuantArgs& a, int64_t bx, int64_t by, ColQuantShared<E>& sh) {
   using S = typename E::S;
   using E8 = EightOf<E>;
@@ -541,20 +542,54 @@ __device__ __forceinline__ void col_quant(const QuantArgs& a, int64_t bx, int64_
   }
   {
     const int jc = threadIdx.x & 63, jr = threadIdx.x >> 6;
-    uint32_t m = 0;
-    float s = 0.f;
-    if (c0 + jc < a.cols) {
+    if (OWN && a.nrb == 0) {
+      // few rows: the block's own statistics, 32 rows at a time, joined over the wave
+      uint32_t m[8];
+      float s[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { m[k] = 0; s[k] = 0.f; }
+      if (c < a.cols) {
 #pragma unroll 4
-      for (int i = jr; i < a.nrb; i += 4) {
-        m = max(m, *gptr(a.part_max + (int64_t)i * a.cols + c0 + jc));
-        if (SUM && first) s += *gptr(a.part_sum + (int64_t)i * a.cols + c0 + jc);
+        for (int64_t r = tr; r < a.rows; r += 32) {
+          float v[8];
+          E::expand(load_end8<E>((const S*)a.x + r * a.ldx, c, a.cols), v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            m[k] = max(m[k], __float_as_uint(v[k]) & 0x7fffffffu);
+            if (SUM) s[k] += v[k];
+          }
+        }
       }
+#pragma unroll
+      for (int off = 8; off <= 32; off <<= 1)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          m[k] = max(m[k], (uint32_t)__shfl_xor((int)m[k], off, 64));
+          if (SUM) s[k] += __shfl_xor(s[k], off, 64);
+        }
+      if (jc < 8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          pm[jr][8 * tc + k] = m[k];
+          if (SUM) ps[jr][8 * tc + k] = s[k];
+        }
+      }
+    } else {
+      uint32_t m = 0;
+      float s = 0.f;
+      if (c0 + jc < a.cols) {
+#pragma unroll 4
+        for (int i = jr; i < a.nrb; i += 4) {
+          m = max(m, *gptr(a.part_max + (int64_t)i * a.cols + c0 + jc));
+          if (SUM && first) s += *gptr(a.part_sum + (int64_t)i * a.cols + c0 + jc);
+        }
+      }
+      pm[jr][jc] = m;
+      if (SUM) ps[jr][jc] = s;
     }
-    pm[jr][jc] = m;
-    if (SUM) ps[jr][jc] = s;
     __syncthreads();
     if (jr == 0) {
-      m = max(max(pm[0][jc], pm[1][jc]), max(pm[2][jc], pm[3][jc]));
+      const uint32_t m = max(max(pm[0][jc], pm[1][jc]), max(pm[2][jc], pm[3][jc]));
       const E8 e(__uint_as_float(m));
       eights[jc] = e;
       if (first && c0 + jc < a.cols) {
@@ -682,15 +717,15 @@ __global__ __launch_bounds__(256) void quant_first_kernel(QuantJobs jobs) {
   }
 }
 
-template <class E>
+template <class E, bool OWN>
 __global__ __launch_bounds__(256) void quant_columns_kernel(QuantJobs jobs) {
   __shared__ ColQuantShared<E> sh;
   int j = 0, b = blockIdx.x;
   while (j + 1 < jobs.n && b >= jobs.blocks[j]) b -= jobs.blocks[j++];
   const QuantArgs& a = jobs.a[j];
   const int gx = (int)((a.cols + 63) / 64);
-  if (a.sum) col_quant<E, true>(a, b % gx, b / gx, sh);
-  else col_quant<E, false>(a, b % gx, b / gx, sh);
+  if (a.sum) col_quant<E, true, OWN>(a, b % gx, b / gx, sh);
+  else col_quant<E, false, OWN>(a, b % gx, b / gx, sh);
 }
 
 // Blocks that take rows: eight a CU, as many as it holds.
@@ -708,7 +743,7 @@ hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
     const QuantArgs& a = jobs.a[j];
     int64_t n;
     if (jobs.columns[j]) {
-      n = (a.cols + 255) / 256 * a.nrb;
+      n = (a.cols + 255) / 256 * a.nrb;  // none, where the tiles do it themselves
       const int k = second.n++;
       second.a[k] = a;
       second.blocks[k] = (int32_t)((a.cols + 63) / 64 * ((a.rows + 127) / 128));
@@ -720,7 +755,7 @@ hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
     first.blocks[j] = (int32_t)n;
     blocks += n;
   }
-  if (blocks > 0) {
+  if (blocks > 0) {  // rows, or statistics
     const unsigned g = (unsigned)blocks;
     if (pieces <= 1) quant_first_kernel<E, 1><<<g, 256, 0, s>>>(first);
     else if (pieces <= 2) quant_first_kernel<E, 2><<<g, 256, 0, s>>>(first);
@@ -732,8 +767,13 @@ hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
   }
   if (second.n) {
     int64_t g = 0;
-    for (int j = 0; j < second.n; ++j) g += second.blocks[j];
-    quant_columns_kernel<E><<<(unsigned)g, 256, 0, s>>>(second);
+    bool own = false;
+    for (int j = 0; j < second.n; ++j) {
+      g += second.blocks[j];
+      own |= second.a[j].nrb == 0;
+    }
+    if (own) quant_columns_kernel<E, true><<<(unsigned)g, 256, 0, s>>>(second);
+    else quant_columns_kernel<E, false><<<(unsigned)g, 256, 0, s>>>(second);
   }
   return hipGetLastError();
 }
@@ -758,11 +798,19 @@ hipError_t launch_quantize_rows(OpType t, const QuantArgs& q, hipStream_t s) {
                         : launch_rows<TF16, QUANT, false>(a, s);
 }
 
-// Row blocks of the columns' statistics: of at least 64 rows, at most 64, and no more than
+// No row blocks where a matrix is laid out alone and has few rows: each tile of 128 rows then
+// takes the statistics itself, reading all rows, and a launch is saved (512 x 8192 bf16: 8.8
+// us, before 11.4; among others, whose first launch is there anyway, it would cost time).
+// Otherwise, row blocks of the columns' statistics: of at least 64 rows, at most 64, and no more than
 // fill the card (kStatBlocks of 256 columns), as each tile of the second kernel reads the
 // statistics of all.
+constexpr int64_t kOwnRows = 512;
 constexpr int64_t kStatBlocks = 1024;  // 8192 x 16384 bf16: 135 us; 512 135, 2048 139, no bound 148
-void quantize_cols_blocks(int64_t rows, int64_t cols, int32_t* nrb, int32_t* rows_per_block) {
+void quantize_cols_blocks(int64_t rows, int64_t cols, bool alone, int32_t* nrb, int32_t* rows_per_block) {
+  if (alone && rows <= kOwnRows) {
+    *nrb = *rows_per_block = 0;
+    return;
+  }
   const int64_t most = kStatBlocks / ((cols + 255) / 256), n = most < 1 ? 1 : most > 64 ? 64 : most;
   int64_t per = (rows + n - 1) / n;
   per = per < 64 ? 64 : per;

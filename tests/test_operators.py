@@ -29,7 +29,7 @@ def changed(base, **kw):
 
 
 Q = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=8, scale=FAKE, stream=None)
-C = dict(x=FAKE, dtype=BF, rows=4, cols=8, ldx=8, q=FAKE, ldq=4, scale=FAKE, sum=None, ws=FAKE, nws=1 << 16, stream=None)
+C = dict(x=FAKE, dtype=BF, rows=2000, cols=8, ldx=8, q=FAKE, ldq=2000, scale=FAKE, sum=None, ws=FAKE, nws=1 << 16, stream=None)
 M = dict(a=FAKE, lda=8, sa=FAKE, b=FAKE, ldb=8, sb=FAKE, bias=None, dtype=BF, out=FAKE, ldo=6, m=4, n=6, k=8, ws=None, nws=0, stream=None)
 N = dict(x=FAKE, ldx=8, res=None, ldres=0, w=FAKE, dtype=BF, rows=4, cols=8, eps=1e-6, h=None, ldh=0, y=FAKE, ldy=8, q=None,
          ldq=0, scale=None, stream=None)
@@ -52,7 +52,7 @@ def test_unknown_type(name):
     ("prm_quantize_rows", dict(rows=1 << 31)), ("prm_quantize_rows", dict(ldx=7)), ("prm_quantize_rows", dict(ldq=7)),
     ("prm_quantize_rows", dict(x=None)), ("prm_quantize_rows", dict(q=None)), ("prm_quantize_rows", dict(scale=None)),
     ("prm_quantize_cols", dict(rows=0)), ("prm_quantize_cols", dict(rows=(1 << 22) + 1, ldq=1 << 30)),
-    ("prm_quantize_cols", dict(ldq=3)), ("prm_quantize_cols", dict(ldx=7)), ("prm_quantize_cols", dict(nws=8)),
+    ("prm_quantize_cols", dict(ldq=1999)), ("prm_quantize_cols", dict(ldx=7)), ("prm_quantize_cols", dict(nws=8)),
     ("prm_quantize_cols", dict(ws=None)), ("prm_quantize_cols", dict(x=None)),
     ("prm_int8_matmul", dict(k=0)), ("prm_int8_matmul", dict(k=(1 << 20) + 1, lda=1 << 21, ldb=1 << 21)),
     ("prm_int8_matmul", dict(k=131072, lda=131073, ldb=131072)),
