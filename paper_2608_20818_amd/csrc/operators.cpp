@@ -211,6 +211,12 @@ at::Tensor with_rows(const at::Tensor& t, Rows* r) {
   return c;
 }
 
+// What a saved tensor's hooks gave back is what was saved.
+void as_saved(const at::Tensor& t, const at::Tensor& like, bool ok) {
+  if (!t.is_cuda() || t.device() != like.device() || t.scalar_type() != like.scalar_type() || !ok)
+    throw std::runtime_error("a saved tensor came back with another type, device or shape");
+}
+
 at::Tensor linear(const at::Tensor& x, const at::Tensor& w, const at::Tensor& bias) {
   Rows rx, rw;
   rows_of(x, &rx);
@@ -235,11 +241,10 @@ struct Linear : torch::autograd::Function<Linear> {
     {
       at::AutoGradMode off(false);
       const variable_list saved = ctx->get_saved_variables();
-      const at::Tensor &x = saved[0], &w = saved[1];
       Rows rg, rx, rw;
-      const at::Tensor gy = with_rows(grads[0], &rg);
-      rows_of(x, &rx);
-      rows_of(w, &rw);
+      const at::Tensor gy = with_rows(grads[0], &rg), x = with_rows(saved[0], &rx), w = with_rows(saved[1], &rw);
+      as_saved(x, gy, rx.rows == rg.rows);
+      as_saved(w, gy, rw.rows == rg.cols && rw.cols == rx.cols);
       if (ctx->needs_input_grad(0)) out[0] = empty(x.sizes(), x.scalar_type(), x);
       if (ctx->needs_input_grad(1)) out[1] = empty(w.sizes(), w.scalar_type(), w);
       if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) out[2] = empty({rw.rows}, w.scalar_type(), w);
@@ -305,15 +310,16 @@ struct Norm : torch::autograd::Function<Norm> {
     {
       at::AutoGradMode off(false);
       const variable_list saved = ctx->get_saved_variables();
-      const at::Tensor &h = saved[0], &w = saved[1];
+      const at::Tensor& w = saved[1];
       const bool need_dw = w.defined() && ctx->needs_input_grad(1), kept = grads.size() > 1 && grads[1].defined();
       at::Tensor dx;
       if (!grads[0].defined()) {  // only the kept sum has a gradient
         dx = kept ? grads[1] : at::Tensor();
       } else {
         Rows rg, rs, rh;
-        const at::Tensor gy = with_rows(grads[0], &rg), gh = kept ? with_rows(grads[1], &rs) : at::Tensor();
-        rows_of(h, &rh);
+        const at::Tensor gy = with_rows(grads[0], &rg), gh = kept ? with_rows(grads[1], &rs) : at::Tensor(), h = with_rows(saved[0], &rh);
+        as_saved(h, gy, h.sizes() == gy.sizes());
+        if (w.defined()) as_saved(w, gy, vector_of(w, gy, gy.scalar_type(), rg.cols));
         dx = empty(h.sizes(), h.scalar_type(), h);
         at::Tensor ws;
         uint64_t need = 0;

@@ -79,8 +79,8 @@ struct ProductArgs {
   int64_t m, n, k, lda, ldb, ldo;
   int32_t* part;     // the splits' sums, or nullptr
 };
-// The kernels, by tile; ANY: rows that start on any byte.  The piped ones (64, 128) can
-// split k over blocks, whose sums meet in `part` (product_workspace bytes), and, as 256, take
+// The kernels, by tile; ANY: rows that start on any byte; PAIRED: two blocks a CU.  64 and 128 can
+// split k over blocks, whose sums meet in `part` (product_workspace bytes), and, as PAIRED and 256, take
 // operands that were laid out anew.
 enum ProductKind : int32_t {
   PRODUCT_FEW = 1, PRODUCT_ANY64, PRODUCT_ANY128, PRODUCT_64, PRODUCT_128, PRODUCT_128_PAIRED, PRODUCT_256,

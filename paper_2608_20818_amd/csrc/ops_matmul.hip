@@ -623,14 +623,14 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs g) {
   *(PRM_GLOBAL u32x4_t*)(g.dst[which] + row * g.kp + k) = v;
 }
 
-template <class E, int BM, int NBUF>
+template <class E, int BM>
 void launch_piped(const ProductArgs& p, int splits, hipStream_t s) {
   const int tm = (int)((p.m + BM - 1) / BM), tn = (int)((p.n + BM - 1) / BM);
   if (splits == 1) {
-    piped_kernel<E, BM, BM, 128, NBUF, false><<<(unsigned)(tm * tn), 256, 0, s>>>(p, tm, tn);
+    piped_kernel<E, BM, BM, 128, 4, false><<<(unsigned)(tm * tn), 256, 0, s>>>(p, tm, tn);
     return;
   }
-  piped_kernel<E, BM, BM, 128, NBUF, true><<<dim3((unsigned)(tm * tn), (unsigned)splits), 256, 0, s>>>(p, tm, tn);
+  piped_kernel<E, BM, BM, 128, 4, true><<<dim3((unsigned)(tm * tn), (unsigned)splits), 256, 0, s>>>(p, tm, tn);
   join_kernel<E><<<(unsigned)((p.m * ((p.n + 7) / 8) + 255) / 256), 256, 0, s>>>(p, splits);
 }
 
@@ -666,9 +666,9 @@ hipError_t launch(ProductArgs p, const ProductPlan& plan, hipStream_t s) {
     case PRODUCT_FEW: few_kernel<E, 8><<<(unsigned)((p.n + 15) / 16), 512, 0, s>>>(p); break;
     case PRODUCT_ANY64: tile_kernel<E, 64, 64, 4><<<tiles, 256, 0, s>>>(p, (int)tm); break;
     case PRODUCT_ANY128: tile_kernel<E, 128, 128, 2><<<tiles, 256, 0, s>>>(p, (int)tm); break;
-    case PRODUCT_64: launch_piped<E, 64, 4>(p, plan.splits, s); break;
-    case PRODUCT_128: launch_piped<E, 128, 4>(p, plan.splits, s); break;
-    case PRODUCT_128_PAIRED: launch_piped<E, 128, 2>(p, plan.splits, s); break;
+    case PRODUCT_64: launch_piped<E, 64>(p, plan.splits, s); break;
+    case PRODUCT_128: launch_piped<E, 128>(p, plan.splits, s); break;
+    case PRODUCT_128_PAIRED: piped_kernel<E, 128, 128, 128, 2, false><<<tiles, 256, 0, s>>>(p, (int)tm, (int)tn); break;
     default: big_kernel<E><<<tiles, 256, 0, s>>>(p, (int)tm, (int)tn);
   }
   return hipGetLastError();
@@ -685,7 +685,7 @@ bool product_takes(const ProductArgs& p, const ProductPlan& plan) {
   if (plan.pack && (kind < PRODUCT_64 || plan.pack > 3)) return false;
   if (plan.splits == 1 ? p.k > kMaxPieceK : plan.splits > 1 && ((pieces + plan.splits - 1) / plan.splits + 1) * 128 > kMaxPieceK)
     return false;  // a piece's sum has to fit 32 bits
-  if (plan.splits != 1 && (kind < PRODUCT_64 || kind == PRODUCT_256 || plan.splits < 1 || plan.splits > pieces || plan.splits > 64))
+  if (plan.splits != 1 && ((kind != PRODUCT_64 && kind != PRODUCT_128) || plan.splits < 1 || plan.splits > pieces || plan.splits > 64))
     return false;
   if (kind == PRODUCT_FEW) return p.m <= 16;
   if (kind == PRODUCT_ANY64 || kind == PRODUCT_ANY128) return true;
