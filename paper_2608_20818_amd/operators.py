@@ -255,6 +255,9 @@ class _RmsNorm(torch.autograd.Function):
         if gy is None:  # only the kept sum has a gradient
             dw = torch.zeros_like(weight) if need_dw else None
             return (gh if ctx.needs_input_grad[0] else None), dw, (gh if ctx.needs_input_grad[2] else None), None
+        _same(h, gy, gy.shape, "saved input")  # hooks may bring back something else
+        if weight is not None:
+            _same(weight, gy, gy.shape[-1:], "saved weight")
         rows, cols = _count(h)
         L = load()
         with _device_of(h) as stream:

@@ -181,3 +181,16 @@ def test_names_are_public():
     for n in ("quantize_rows", "int8_matmul", "int8_linear", "rms_norm"):
         assert n in prm.__all__ and callable(getattr(prm, n))
     assert ctypes.sizeof(ctypes.c_int32) == 4
+
+
+@pytest.mark.parametrize("h,w", [((3, 7), (8,)), ((2, 8), (8,)), ((3, 8), (7,)), ((3, 8), None)], ids=str)
+def test_saved_norm_inputs_are_checked(h, w):
+    # what hooks bring back reaches the gradient's kernel only in the shape and type saved
+    from types import SimpleNamespace
+
+    from paper_2608_20818_amd import operators
+    t = torch.float16 if w is None else torch.float32
+    ctx = SimpleNamespace(saved_tensors=(torch.zeros(h, dtype=t), torch.zeros(w) if w else None), needs_input_grad=(True, w is not None, False, False),
+                          eps=1e-6)
+    with pytest.raises(ValueError, match="saved (input|weight)"):
+        operators._RmsNorm.backward(ctx, torch.zeros(3, 8))
