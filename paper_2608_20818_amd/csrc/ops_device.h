@@ -164,9 +164,9 @@ __device__ __forceinline__ void store_q8(int8_t* row, int64_t c, int64_t cols, c
 // most, and u by 2^-24 (fp32 products: none): 127 * 4 * 2^-24 = 3.1e-5, so where the
 // remainder stays 4e-5 clear of 1/2 the number is right.
 //
-// Otherwise, and in rows too small or too large for fp32, comparing 254 |u| with
-// (2 k + 1) top decides, in a type that holds both exactly: fp32 (24 bits) but for WIDE,
-// which takes fp64 (products of fp32 values: to its last bit).
+// Otherwise comparing 254 |u| with (2 k + 1) top decides, in a type that holds both exactly:
+// fp32 (24 bits; 255 top is in its range up to 1.3e36) but for WIDE and rows too small or too
+// large for that, which take fp64 (products of fp32 values: to its last bit).
 // 16384 x 4096 bf16 rows: 34 us; with a check for each value 38, for each 8 values 45
 // (values on a border, half the largest above all, are common there).
 enum EightKind { VALUES, PRODUCT32, WIDE };
@@ -178,7 +178,7 @@ struct Eight {
   bool fp32;  // fp32 decides: always (VALUES), or where it can
   Eight() = default;
   __device__ __forceinline__ explicit Eight(U t) : top(t) {
-    fp32 = t > (U)1e-35f && t < (U)3e38f;
+    fp32 = t > (U)1e-35f && t < (U)1e36f;
     inv = fp32 ? 127.f / (float)t : 0.f;
     if (fmaf(inv, (float)t, -127.f) < 0.f && fp32) inv = __uint_as_float(__float_as_uint(inv) + 1);
     if constexpr (K == VALUES) fp32 = fp32 && ((__float_as_uint(t) & 0x7fffffu) | 0x800000u) % 127u != 0;
