@@ -399,7 +399,8 @@ int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_
  *   y = h * w / sqrt(mean(h^2) + eps)    (w: cols values, NULL: ones)
  * written either to y (type dtype; q and scale NULL) or to q and scale in 8 bits
  * (y NULL), as the quantiser would lay out the unrounded y.  The norm is that of the
- * rounded h.  eps > 0.  The sum of squares is taken in fp32. */
+ * rounded h.  eps > 0.  The sum of squares is taken in fp32, and in fp64 in rows whose
+ * squares leave fp32's range. */
 int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres, const void* w,
                  int32_t dtype, int64_t rows, int64_t cols, float eps, void* h, int64_t ldh,
                  void* y, int64_t ldy, int8_t* q, int64_t ldq, float* scale, void* hip_stream);

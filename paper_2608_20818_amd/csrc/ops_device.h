@@ -207,8 +207,8 @@ struct Eight {
   }
   __device__ __forceinline__ bool sure(float rest) const { return K == VALUES ? fp32 : fp32 && rest < 0.49996f; }
   // the scale: factor * top / 127; a row with a value that is not finite has NaN
-  __device__ __forceinline__ float scale(float factor) const {
-    return finite() ? (float)((double)factor * (double)top / 127.0) : __builtin_nanf("");
+  __device__ __forceinline__ float scale(double factor) const {
+    return finite() ? (float)(factor * (double)top / 127.0) : __builtin_nanf("");
   }
 };
 // the rounding of a type's own values

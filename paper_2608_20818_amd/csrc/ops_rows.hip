@@ -31,6 +31,12 @@ __device__ __forceinline__ double wave_max(double v) {
   for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
   return v;
 }
+using prm::wave_sum;  // of floats
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
 
 // The largest |u|, that keeps a NaN: fp32 magnitudes as their bits (NaN above infinity
 // above the finite ones), fp64 ones with a flag in the place of NaN (infinity).
@@ -47,8 +53,8 @@ template <> struct Top<double> {
 };
 
 // Sum, and largest, over the threads of a row: a wave, or the whole block.
-template <int TPR, typename U>
-__device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_sum, bool with_top, float* rs, decltype(Top<U>::m)* rt) {
+template <int TPR, typename T, typename U>
+__device__ __forceinline__ void row_reduce(T& ss, Top<U>& top, bool with_sum, bool with_top, T* rs, decltype(Top<U>::m)* rt) {
   if (with_sum) ss = wave_sum(ss);
   if (with_top) top.m = wave_max(top.m);
   if constexpr (TPR > 64) {
@@ -58,7 +64,7 @@ __device__ __forceinline__ void row_reduce(float& ss, Top<U>& top, bool with_sum
       if (with_top) rt[w] = top.m;
     }
     __syncthreads();
-    ss = 0.f;
+    ss = 0;
 #pragma unroll
     for (int i = 0; i < TPR / 64; ++i) {
       ss += rs[i];
@@ -91,7 +97,8 @@ enum { NORM = 0, NORM8 = 1, QUANT = 2 };
 template <class E, int TPR, int NCH, int MODE, bool RES>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a) {
   using S = typename E::S;
-  // the product h w of two 16-bit values is exact in fp32, that of fp32 values in fp64
+  // the product h w of two 16-bit values is exact in fp32 (of bf16: within its range), that of fp32
+  // values in fp64
   using U = std::conditional_t<MODE == NORM8 && sizeof(S) == 4, double, float>;
   constexpr int WPB = TPR == 64 ? 1 : TPR / 64;
   __shared__ float rs[WPB];
@@ -161,7 +168,65 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_kernel(NormArgs a)
     for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, sum8(c));
   }
   if constexpr (MODE == QUANT) top.m = raw_top.bits();
-  row_reduce<TPR, U>(ss, top, MODE != QUANT, MODE != NORM, rs, rt);
+  row_reduce<TPR>(ss, top, MODE != QUANT, MODE != NORM, rs, rt);
+  // Rows whose squares leave fp32's range, or whose products of bf16 values do, at either end:
+  // once more in fp64, from memory (the kept sum is read back by the thread that wrote it), so
+  // that the other rows' registers hold none of it.
+  if constexpr (MODE != QUANT && !std::is_same_v<E, TF16>) {
+    bool far = !(ss < __builtin_huge_valf());
+    if (MODE == NORM8 && sizeof(S) == 2) far |= !(top.value() > (U)1e-35f && top.value() < (U)1e36f);
+    if (far) {
+      __shared__ double ds[WPB], dt[WPB];
+      const S* h = RES ? hrow : x;
+      if (MODE == NORM8 && top.value() == (U)0) {
+        // a row of zeros, as padding is (8192 x 5120: 57 us; through the products 72), or products
+        // below fp32's range
+        TopRaw<E> some;
+#pragma clang loop unroll(disable)
+        for (int64_t c = 8 * t; c < cols; c += 8 * TPR) some.add(load_row8<E>(h, c, cols));
+        if (!(TPR == 64 ? __any(some.bits() != 0) : __syncthreads_or(some.bits() != 0))) {
+#pragma clang loop unroll(disable)
+          for (int64_t c = 8 * t; c < cols; c += 8 * TPR) store_q8(a.q + row * a.ldq, c, cols, u32x2b_t{0u, 0u});
+          if (t == 0) a.scale[row] = 0.f;
+          return;
+        }
+      }
+      double sum = 0;
+      Top<double> most;
+#pragma clang loop unroll(disable)
+      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
+        float v[8], f[8];
+        E::expand(load_row8<E>(h, c, cols), v);
+        weight8(c, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          sum += (double)v[k] * v[k];
+          if (MODE == NORM8) most.add((double)v[k] * f[k]);
+        }
+      }
+      row_reduce<TPR>(sum, most, true, MODE == NORM8, ds, dt);
+      const double root = 1.0 / sqrt(sum / (double)cols + (double)a.eps);
+      const Eight<double, WIDE> eight(most.value());
+      if (MODE == NORM8 && t == 0) a.scale[row] = eight.scale(root);
+#pragma clang loop unroll(disable)
+      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
+        float v[8], f[8];
+        E::expand(load_row8<E>(h, c, cols), v);
+        weight8(c, f);
+        if constexpr (MODE == NORM) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = (float)((double)v[k] * root * f[k]);
+          store_row8<E>((S*)a.y + row * a.ldy, c, cols, E::pack(v));
+        } else {
+          double u[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) u[k] = (double)v[k] * f[k];
+          store_q8(a.q + row * a.ldq, c, cols, eight8(eight, u));
+        }
+      }
+      return;
+    }
+  }
   const float r = MODE == QUANT ? 1.f : 1.f / sqrtf(ss / (float)cols + a.eps);
   using R = std::conditional_t<MODE == QUANT, EightOf<E>, Eight<U, std::is_same_v<E, TBF16> ? PRODUCT32 : WIDE>>;
   const R eight(top.value());

@@ -65,3 +65,64 @@ def test_norm_eight_bits_of_large_products():
     qe, se = eight(x.double() * w.double())
     assert torch.equal(q.cpu().double(), qe)
     check_scale(s, se * r[:, 0], (sums(12) / 2 + 6) * U)
+
+
+WIDE = [(1, 40), (3, 513), (5, 1001), (600, 2050), (2, 4100), (2, 12289), (2, 33000)]
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32], ids=NAMES.get)
+@pytest.mark.parametrize("shape", WIDE, ids=str)
+def test_norm_past_the_range_of_squares(shape, t):
+    # rows whose squares leave fp32's range beside ordinary ones, plain and in 8 bits, with products
+    # h w that leave it at either end too
+    x, res = rand(shape, t, 1), rand(shape, t, 2)
+    up = torch.tensor([2.0 ** e for e in (70, 0, 100, 120, 63)], dtype=torch.float64)
+    by = up[torch.arange(shape[0]) % 5][:, None]
+    x, res = (x.double() * by).to(t), (res.double() * by).to(t)
+    for scale in (1.0, 2.0 ** 60, 2.0 ** -120):
+        w = rand(shape[1:], t, 3, scale)
+        for rs in (None, res):
+            h, r, y = norm64(x, rs, w, 1e-6, t)
+            got = prm.rms_norm(x.cuda(), w.cuda(), None if rs is None else rs.cuda())
+            got8 = prm.rms_norm(x.cuda(), w.cuda(), None if rs is None else rs.cuda(), quantize=True)
+            if rs is not None:
+                assert torch.equal(got[1], got8[2])
+                h, r, y = norm64(got[1].cpu(), None, w, 1e-6, t)
+                got = got[0]
+            check(got, y, ((sums(shape[1]) / 2 + 6) * U + half(t)) * y.abs() * (1 + half(t)) + low(t))
+            qe, se = eight(h * w.double())
+            assert torch.equal(got8[0].cpu().double(), qe)
+            check_scale(got8[1], se * r[:, 0], (sums(shape[1]) / 2 + 6) * U)
+
+
+def test_norm_eight_bits_of_small_products():
+    # h w below fp32's normal range: q is decided on the exact products all the same
+    t = torch.bfloat16
+    x, w = rand((4, 300), t, 4), rand((300,), t, 5, 2.0 ** -60)
+    x = (x.double() * torch.tensor([2.0 ** -60, 2.0 ** -70, 2.0 ** -80, 1.0], dtype=torch.float64)[:, None]).to(t)
+    q, s = prm.rms_norm(x.cuda(), w.cuda(), eps=1e-30, quantize=True)
+    qe, se = eight(x.double() * w.double())
+    r = 1 / torch.sqrt(x.double().square().mean(1) + float(torch.tensor(1e-30)))
+    assert torch.equal(q.cpu().double(), qe)
+    check_scale(s, se * r, (sums(300) / 2 + 6) * U)
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32], ids=NAMES.get)
+def test_norm_of_rows_that_are_not_finite_beside_large_ones(t):
+    x, w = rand((6, 700), t, 6), rand((700,), t, 7)
+    x[0] *= 2.0 ** 80
+    x[1] *= 2.0 ** 80
+    x[1, 5] = float("nan")
+    x[2] *= 2.0 ** 80
+    x[2, 699] = float("-inf")
+    x[3] = 0
+    x[4, 7] = 2.0 ** 120
+    y, (q, s) = prm.rms_norm(x.cuda(), w.cuda()).cpu(), (v.cpu() for v in prm.rms_norm(x.cuda(), w.cuda(), quantize=True))
+    assert torch.isnan(y[1]).all() and torch.isnan(y[2, 699]) and (y[2, :699] == 0).all() and (y[3] == 0).all()
+    assert torch.isnan(s[1:3]).all() and (q[1:4] == 0).all() and s[3] == 0
+    rows = [0, 4, 5]
+    _, r, want = norm64(x[rows], None, w, 1e-6, t)
+    check(y[rows], want, ((sums(700) / 2 + 6) * U + half(t)) * want.abs() * (1 + half(t)) + low(t))
+    qe, se = eight(x[rows].double() * w.double())
+    assert torch.equal(q[rows].double(), qe)
+    check_scale(s[rows], se * r[:, 0], (sums(700) / 2 + 6) * U)
