@@ -410,7 +410,8 @@ int prm_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldres
  *   dx = r (g - n mean(g n)) + gh      (gh: the gradient of the kept sum, or NULL;
  *                                       dx is the residual's gradient too)
  *   dw = sum over rows of gy n         (or dw NULL)
- * both of type dtype; dw is added in fp32 in a fixed order.  `workspace`:
+ * both of type dtype; sums in fp32 (of h scaled down in rows whose sums leave its range),
+ * dw added in a fixed order.  `workspace`:
  * prm_rms_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, used by this
  * call only (may be NULL without dw).  rows = 0 writes dw = 0. */
 uint64_t prm_rms_norm_backward_workspace(int64_t rows, int64_t cols);

@@ -320,7 +320,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
   __shared__ float red[2][2][WPB];
   __shared__ float share[TPR == 64 ? 4 : 1][TPR == 64 ? 512 : 1];
   static_assert(TPR > 64 || NCH == 1, "the share of a wave");
-  const int t = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
+  int t = TPR == 64 ? (threadIdx.x & 63) : threadIdx.x;
   const int wave = threadIdx.x >> 6;
   const int64_t cols = a.cols;
   const int64_t step = (int64_t)gridDim.x * (TPR == 64 ? 4 : 1);
@@ -355,47 +355,31 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
       }
     }
   };
-  int64_t row = TPR == 64 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
-  if (AHEAD && row < a.rows) fetch(row);
-  for (; row < a.rows; row += step) {
-    const S* gy = (const S*)a.gy + row * a.ldgy;
-    const S* h = (const S*)a.h + row * a.ldh;
-    const S* gh = a.gh ? (const S*)a.gh + row * a.ldgh : nullptr;
-    S* dx = (S*)a.dx + row * a.lddx;
-    float ss = 0.f, sg = 0.f;  // sums of h^2 and of g h
-    auto stats = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg) __attribute__((always_inline)) {
-      float v[8], g[8], f[8];
-      E::expand(xh, v);
-      E::expand(xg, g);
-      weight8(c, f);
+  // sums of h^2 and of g h of a piece, h scaled by `down`; fma by name, as both loops below have
+  // to come to the same bits
+  auto stats = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, float down, float& ss, float& sg) __attribute__((always_inline)) {
+    float v[8], g[8], f[8];
+    E::expand(xh, v);
+    E::expand(xg, g);
+    weight8(c, f);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        ss += v[k] * v[k];
-        sg += g[k] * f[k] * v[k];
-      }
-    };
-    typename E::Raw ch[N], cg[N], cs[N];
-    if constexpr (NCH) {
-      if (!AHEAD) fetch(row);
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        ch[i] = rh[i];
-        cg[i] = rg[i];
-        if (a.gh) cs[i] = rs[i];
-      }
-      if (AHEAD && row + step < a.rows) fetch(row + step);
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int64_t c = 8 * ((int64_t)i * TPR + t);
-        if (c < cols) stats(c, ch[i], cg[i]);
-      }
-    } else {
-      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) stats(c, load_row8<E>(h, c, cols), load_row8<E>(gy, c, cols));
+    for (int k = 0; k < 8; ++k) {
+      v[k] *= down;
+      ss = fmaf(v[k], v[k], ss);
+      sg = fmaf(g[k] * f[k], v[k], sg);
     }
+  };
+  auto swept = [&](int64_t row, float down, float& ss, float& sg) __attribute__((always_inline)) {
+    ss = sg = 0.f;
+#pragma clang loop unroll(disable)
+    for (int64_t c = 8 * t; c < cols; c += 8 * TPR)
+      stats(c, load_row8<E>((const S*)a.h + row * a.ldh, c, cols), load_row8<E>((const S*)a.gy + row * a.ldgy, c, cols), down, ss, sg);
+  };
+  auto joined = [&](float& ss, float& sg) __attribute__((always_inline)) {
     ss = wave_sum(ss);
     sg = wave_sum(sg);
     if constexpr (TPR > 64) {
-      // two sets of slots in turn: a wave writes the next row's behind one barrier only
+      // two sets of slots in turn: a wave writes the next sums behind one barrier only
       if ((threadIdx.x & 63) == 0) {
         red[flip][0][wave] = ss;
         red[flip][1][wave] = sg;
@@ -409,42 +393,110 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
       }
       flip ^= 1;
     }
+  };
+  // a piece of dx, and its share of dw (`with_dw`); r and coef = mean(g n) r are those of h scaled
+  auto out = [&](int64_t row, int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, const typename E::Raw& xs, float r, float coef, float down,
+                 bool with_dw, float d[8]) __attribute__((always_inline)) {
+    float v[8], g[8], f[8], o[8];
+    E::expand(xh, v);
+    E::expand(xg, g);
+    weight8(c, f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      v[k] *= down;
+      d[k] = with_dw ? d[k] + g[k] * (v[k] * r) : d[k];
+      o[k] = r * down * (g[k] * f[k] - v[k] * coef);
+    }
+    if (a.gh) {
+      E::expand(xs, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] += v[k];
+    }
+    store_row8<E>((S*)a.dx + row * a.lddx, c, cols, E::pack(o));
+  };
+  auto out_swept = [&](int64_t row, int64_t c, float r, float coef, float down, bool with_dw, float d[8]) __attribute__((always_inline)) {
+    const typename E::Raw xh = load_row8<E>((const S*)a.h + row * a.ldh, c, cols);
+    out(row, c, xh, load_row8<E>((const S*)a.gy + row * a.ldgy, c, cols), a.gh ? load_row8<E>((const S*)a.gh + row * a.ldgh, c, cols) : xh, r, coef, down,
+        with_dw, d);
+  };
+  // NCH 0: dw of the row's pieces in `part` itself
+  auto out_long = [&](int64_t row, float r, float coef, float down, bool with_dw) __attribute__((always_inline)) {
+    for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
+      float d[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[k] = first || c + k >= cols || !a.dw ? 0.f : mine[c + k];
+      out_swept(row, c, r, coef, down, with_dw, d);
+      if (a.dw)
+        for (int k = 0; k < 8 && c + k < cols; ++k) mine[c + k] = d[k];
+    }
+    first = false;
+  };
+  const int64_t row0 = TPR == 64 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  int64_t row = row0;
+  float far = 0.f;  // NaN once a row's sums have left fp32's range
+  if (AHEAD && row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
+    float ss = 0.f, sg = 0.f;
+    typename E::Raw ch[N], cg[N], cs[N];
+    if constexpr (NCH) {
+      if (!AHEAD) fetch(row);
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        ch[i] = rh[i];
+        cg[i] = rg[i];
+        if (a.gh) cs[i] = rs[i];
+      }
+      if (AHEAD && row + step < a.rows) fetch(row + step);
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int64_t c = 8 * ((int64_t)i * TPR + t);
+        if (c < cols) stats(c, ch[i], cg[i], 1.f, ss, sg);
+      }
+    } else {
+      swept(row, 1.f, ss, sg);
+    }
+    joined(ss, sg);
+    if (!std::is_same_v<E, TF16>) far = fmaf(ss, 0.f, fmaf(sg, 0.f, far));
     const float r = 1.f / sqrtf(ss / (float)cols + a.eps);
-    const float coef = r * r * (sg / (float)cols);  // mean(g n) r: what each h is scaled by
-    auto out = [&](int64_t c, const typename E::Raw& xh, const typename E::Raw& xg, const typename E::Raw& xs, float d[8]) __attribute__((always_inline)) {
-      float v[8], g[8], f[8], o[8];
-      E::expand(xh, v);
-      E::expand(xg, g);
-      weight8(c, f);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        d[k] += g[k] * (v[k] * r);
-        o[k] = r * (g[k] * f[k] - v[k] * coef);
-      }
-      if (a.gh) {
-        E::expand(xs, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] += v[k];
-      }
-      store_row8<E>(dx, c, cols, E::pack(o));
-    };
+    const float coef = r * r * (sg / (float)cols);
     if constexpr (NCH) {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int64_t c = 8 * ((int64_t)i * TPR + t);
-        if (c < cols) out(c, ch[i], cg[i], cs[i], dw[i]);
+        if (c < cols) out(row, c, ch[i], cg[i], cs[i], r, coef, 1.f, true, dw[i]);
       }
     } else {
-      for (int64_t c = 8 * t; c < cols; c += 8 * TPR) {
-        float d[8];
+      out_long(row, r, coef, 1.f, true);
+    }
+  }
+  // Rows whose sums left fp32's range, once more, h scaled by a power of two: an infinite sum of
+  // squares gave r = 0, so such a row has no share of dw yet, one that has an infinite sum of g h
+  // alone has.  A loop of its own, as in the first one its registers cost the others a wave of four,
+  // and a branch 8% (8192 x 1024 bf16: 20.8 us, 22.4).
+  if (!std::is_same_v<E, TF16> && !(far == 0.f)) {
+    constexpr float inf = __builtin_huge_valf();
+    asm volatile("" : "+v"(t));  // nothing that is computed from it is held through the first loop
+#pragma clang loop unroll(disable)
+    for (row = row0; row < a.rows; row += step) {
+      float ss, sg;
+      swept(row, 1.f, ss, sg);
+      joined(ss, sg);
+      if (ss < inf && fabsf(sg) < inf) continue;
+      const bool with_dw = !(ss < inf);
+      constexpr float down = 0x1p-64f;
+      swept(row, down, ss, sg);
+      joined(ss, sg);
+      const float r = 1.f / sqrtf(ss / (float)cols + a.eps * down * down);
+      const float coef = r * r * (sg / (float)cols);
+      if constexpr (NCH) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = first || c + k >= cols || !a.dw ? 0.f : mine[c + k];
-        const typename E::Raw xh = load_row8<E>(h, c, cols);
-        out(c, xh, load_row8<E>(gy, c, cols), gh ? load_row8<E>(gh, c, cols) : xh, d);
-        if (a.dw)
-          for (int k = 0; k < 8 && c + k < cols; ++k) mine[c + k] = d[k];
+        for (int i = 0; i < NCH; ++i) {
+          const int64_t c = 8 * ((int64_t)i * TPR + t);
+          if (c < cols) out_swept(row, c, r, coef, down, with_dw, dw[i]);
+        }
+      } else {
+        out_long(row, r, coef, down, with_dw);
       }
-      first = false;
     }
   }
   if (!a.dw) return;

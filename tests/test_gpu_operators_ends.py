@@ -126,3 +126,73 @@ def test_norm_of_rows_that_are_not_finite_beside_large_ones(t):
     qe, se = eight(x[rows].double() * w.double())
     assert torch.equal(q[rows].double(), qe)
     check_scale(s[rows], se * r[:, 0], (sums(700) / 2 + 6) * U)
+
+
+def additions(rows, cols, t):
+    # of dw, by the kernel's rule: a thread's rows one after the other, the four waves of a block of
+    # short rows, each 32nd of the blocks' sums, and 32 of those
+    groups = -(-rows // 4) if cols <= 512 else rows
+    most = 256 if cols > 4096 else 512 if cols > 2048 and t == torch.float32 else 1024
+    blocks = min(groups, most)
+    return -(-groups // blocks) + 4 + -(-blocks // 32) + 32
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32], ids=NAMES.get)
+@pytest.mark.parametrize("shape", WIDE, ids=str)
+def test_norm_gradients_past_the_range_of_squares(shape, t):
+    # the rows as above; gradients of about the norm's own size, so that r g stays a normal number.
+    # A value below 2^-62 of a row scaled by 2^-64 may round in fp32's lowest range: 2^-150 of it,
+    # times r 2^64 <= 2^12: below 2^-138 |gy| in n
+    x = rand(shape, t, 8)
+    up = torch.tensor([2.0 ** e for e in (70, 0, 100, 120, 63)], dtype=torch.float64)
+    by = up[torch.arange(shape[0]) % 5][:, None]
+    x, w, gy, gh = (x.double() * by).to(t), rand(shape[1:], t, 9), rand(shape, t, 10), rand(shape, t, 11)
+    for kept in (False, True):
+        xg, wg, rg = x.cuda().requires_grad_(), w.cuda().requires_grad_(), torch.zeros_like(x).cuda()
+        if kept:
+            got = torch.autograd.grad(prm.rms_norm(xg, wg, rg), (xg, wg), (gy.cuda(), gh.cuda()))
+        else:
+            got = torch.autograd.grad(prm.rms_norm(xg, wg), (xg, wg), gy.cuda())
+        h = x.double()
+        r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6)
+        g, n = gy.double() * w.double(), h * r
+        dx = r * (g - n * (g * n).mean(1, keepdim=True))
+        size = r * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+        if kept:
+            dx, size = dx + gh.double(), size + gh.double().abs()
+        s = sums(shape[1])
+        check(got[0], dx, (2.5 * s + 20) * U * size + half(t) * dx.abs() * (1 + 1e-3) + low(t))
+        dw, size = (gy.double() * n).sum(0), (gy.double() * n).abs().sum(0)
+        check(got[1], dw, (s / 2 + 6 + additions(*shape, t)) * U * size + half(t) * dw.abs() * (1 + 1e-3) + low(t)
+              + 2.0 ** -138 * gy.double().abs().sum(0))
+
+
+@pytest.mark.parametrize("shape", [(7, 40), (1030, 2050), (300, 4100), (5, 33000)], ids=str)
+def test_norm_gradients_past_the_range_of_g_h(shape):
+    # squares in fp32's range, sums of g h not (and none of the share of dw twice); rows that are
+    # not finite keep to themselves
+    t, rows = torch.float32, shape[0]
+    x, w, gy = rand(shape, t, 12), rand(shape[1:], t, 13), rand(shape, t, 14)
+    x[1] *= 2.0 ** 55
+    gy[1] *= 2.0 ** 90
+    for bad in (None, float("inf"), float("nan")):
+        xb, gb = x.clone(), gy.clone()
+        if bad is not None:
+            gb[rows - 2, 3], xb[rows - 3, 5] = bad, bad
+        xg, wg = xb.cuda().requires_grad_(), w.cuda().requires_grad_()
+        got = torch.autograd.grad(prm.rms_norm(xg, wg), (xg, wg), gb.cuda())
+        h = x.double()
+        r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6)
+        g, n = gy.double() * w.double(), h * r
+        dx = r * (g - n * (g * n).mean(1, keepdim=True))
+        size = r * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+        s = sums(shape[1])
+        ok = torch.ones(rows, dtype=torch.bool)
+        if bad is not None:
+            ok[[rows - 2, rows - 3]] = False
+            assert not torch.isfinite(got[0][rows - 2]).any() and torch.isnan(got[0][rows - 3, 5])
+            assert not torch.isfinite(got[1][3]) and not torch.isfinite(got[1][5])
+        else:
+            size_w = (gy.double() * n).abs().sum(0)
+            check(got[1], (gy.double() * n).sum(0), (s / 2 + 6 + additions(*shape, t)) * U * size_w + half(t) * size_w + low(t))
+        check(got[0].cpu()[ok], dx[ok], ((2.5 * s + 20) * U * size + half(t) * dx.abs() * (1 + 1e-3) + low(t))[ok])
