@@ -5,18 +5,20 @@
 // Every function returns what the operator does (with the gradients' node, where one is
 // to be recorded), a negative PRM_E* code that libprm gave (the caller raises it), or None:
 // not a plain call (a tensor subclass, another device than the current one, a layout
-// that needs a copy, a type or shape that is wrong), and the Python binding then takes or
-// refuses it.
+// that needs a copy, a type or shape that is wrong, a tracer or a forward-mode tangent), and
+// the Python binding then takes or refuses it.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <cstdint>
 
@@ -27,15 +29,18 @@ namespace {
 PyObject* g_parameter = nullptr;  // torch.nn.Parameter
 
 // A strided device tensor whose metadata and pointer are its own: no subclass (those
-// answer for themselves in Python), no functional transform's wrapper.
+// answer for themselves in Python), no functional transform's wrapper, no tangent; and no tracer,
+// which would record the outputs' allocation alone.
 const at::Tensor* plain(PyObject* o) {
+  if (torch::jit::tracer::isTracing() || c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY)) return nullptr;
   if (!THPVariable_CheckExact(o) && (PyObject*)Py_TYPE(o) != g_parameter) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || !t.is_cuda() || !t.has_storage() || t.layout() != at::kStrided) return nullptr;
   if (t.key_set().has_any(c10::DispatchKeySet({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched,
                                                c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Functionalize,
                                                c10::DispatchKey::Conjugate, c10::DispatchKey::Negative,
-                                               c10::DispatchKey::ZeroTensor})))
+                                               c10::DispatchKey::ZeroTensor})) ||
+      t._fw_grad(0).defined())
     return nullptr;
   return &t;
 }

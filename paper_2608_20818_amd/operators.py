@@ -10,10 +10,14 @@ whose rows are not contiguous is copied first).
 The 8-bit form of a matrix is a pair: int8 ``q`` and a float32 ``scale`` for each of its
 rows, ``s = max|v| / 127``, ``q = rn(127 v / max|v|)``.  A row of zeros has scale 0, a row
 with an infinity or a NaN has scale NaN.
+
+Gradients are those of backward passes.  Forward-mode derivatives, and traces (``torch.jit.trace``,
+``make_fx``), do not see what runs here: both are refused.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import BF16, F16, F32, _check, load
 
@@ -39,6 +43,17 @@ def _float_code(x, what):
 def _on_device(x, what):
     if not x.is_cuda:
         raise ValueError(f"{what}: need a device tensor, got one on {x.device}")
+
+
+def _seen(call, *inputs):
+    """Refuses what would be lost without a word: a call under a tracer, which records the outputs'
+    allocation alone, and inputs with a tangent."""
+    if torch.jit.is_tracing() or torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None:
+        raise RuntimeError(f"{call}: a trace does not see its kernels; call it outside of one")
+    if forward_ad._current_level >= 0:
+        for x in inputs:
+            if isinstance(x, torch.Tensor) and forward_ad.unpack_dual(x).tangent is not None:
+                raise RuntimeError(f"{call}: no forward-mode derivative")
 
 
 def _same(x, like, shape, what):
@@ -108,10 +123,12 @@ def quantize_rows(x, transpose: bool = False):
         r = _native.quantize_cols(x)
         if r is not None:
             return r if type(r) is tuple else _check(r)
+        _seen("quantize_rows")
         return _quantize_cols(x, False)[:2]
     r = _native.quantize_rows(x)
     if r is not None:
         return r if type(r) is tuple else _check(r)
+    _seen("quantize_rows")
     _on_device(x, "x")
     code = _float_code(x, "x")
     x = x.detach()
@@ -154,6 +171,7 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     r = _native.int8_matmul(a, a_scale, b, b_scale, bias, _CODE.get(dtype, -1))
     if r is not None:
         return _check(r) if type(r) is int else r
+    _seen("int8_matmul")
     for t, what in ((a, "a"), (b, "b")):
         _on_device(t, what)
         if t.dtype != torch.int8:
@@ -288,6 +306,7 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
     r = _native.rms_norm(x, weight, residual, eps, quantize)
     if r is not None:
         return _check(r) if type(r) is int else r
+    _seen("rms_norm", x, weight, residual)
     _on_device(x, "x")
     _float_code(x, "x")
     _, cols = _count(x)
@@ -348,6 +367,7 @@ def int8_linear(x, weight, bias=None):
     r = _native.int8_linear(x, weight, bias)
     if r is not None:
         return _check(r) if type(r) is int else r
+    _seen("int8_linear", x, weight, bias)
     _on_device(x, "x")
     _float_code(x, "x")
     _, k = _count(x)

@@ -196,3 +196,28 @@ def test_norm_gradients_past_the_range_of_g_h(shape):
             size_w = (gy.double() * n).abs().sum(0)
             check(got[1], (gy.double() * n).sum(0), (s / 2 + 6 + additions(*shape, t)) * U * size_w + half(t) * size_w + low(t))
         check(got[0].cpu()[ok], dx[ok], ((2.5 * s + 20) * U * size + half(t) * dx.abs() * (1 + 1e-3) + low(t))[ok])
+
+
+# ---------------------------------------------------------------- what autograd may hand over
+def test_forward_mode_and_tracing_are_refused(path):
+    # no tangent is dropped, and no trace records the outputs' allocation alone
+    import torch.autograd.forward_ad as fw
+    from torch.fx.experimental.proxy_tensor import make_fx
+    x, w, nw = rand((4, 16), torch.float32, 20).cuda(), rand((8, 16), torch.float32, 21).cuda(), rand((16,), torch.float32, 22).cuda()
+    q, s = prm.quantize_rows(x)
+    calls = [lambda v: prm.rms_norm(v, nw), lambda v: prm.rms_norm(x, nw, residual=v), lambda v: prm.rms_norm(v, quantize=True)[1],
+             lambda v: prm.int8_linear(v, w), lambda v: prm.int8_linear(w, v)]
+    with fw.dual_level():
+        d = fw.make_dual(x, torch.ones_like(x))
+        for f in calls:
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                f(d)
+    for f in calls[:2] + calls[3:]:
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            torch.func.jvp(f, (x,), (torch.ones_like(x),))
+    for f in calls + [lambda v: prm.quantize_rows(v)[1], lambda v: prm.quantize_rows(v, transpose=True)[1],
+                      lambda v: prm.int8_matmul(q, s, q, s, bias=v[:, 0], dtype=torch.float32)]:
+        with pytest.raises(RuntimeError, match="trace"):
+            torch.jit.trace(f, (x,), check_trace=False)
+        with pytest.raises(RuntimeError, match="trace"):
+            make_fx(f)(x)
