@@ -27,6 +27,7 @@
 namespace {
 
 PyObject* g_parameter = nullptr;  // torch.nn.Parameter
+constexpr int64_t kMaxLayer = 1 << 20;  // tokens and outputs of prm_int8_linear
 
 // A strided device tensor whose metadata and pointer are its own: no subclass (those
 // answer for themselves in Python), no functional transform's wrapper, no tangent; and no tracer,
@@ -273,6 +274,8 @@ PyObject* int8_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
         w->scalar_type() != x->scalar_type() || w->device() != x->device() || !rows_of(*x, &rx) || !rows_of(*w, &rw) || rx.cols != rw.cols ||
         (bias && !vector_of(*bias, *x, x->scalar_type(), rw.rows)))
       Py_RETURN_NONE;
+    // more than prm_int8_linear takes in one call (its gradients' sums among them): from its parts
+    if (rx.rows > kMaxLayer || rw.rows > kMaxLayer) Py_RETURN_NONE;
     const Maybe b = maybe(bias);
     return wrap(records(x) || records(w) || records(bias) ? Linear::apply(*x, *w, b) : linear(*x, *w, or_none(b)));
   });

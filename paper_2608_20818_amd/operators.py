@@ -361,8 +361,9 @@ def int8_linear(x, weight, bias=None):
     each token, ``weight`` ``[n, k]`` for each output channel, all of one type, which the
     result ``[..., n]`` has.  Its gradients are those of the unquantised layer, their
     products in 8 bits too, each operand quantised along the sum it enters:
-    ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T`` (at most 2^20 tokens),
-    ``dbias`` the sum of ``gy`` in fp32.  Each rounding to 8 bits is off by at most half of
+    ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T``, ``dbias`` the sum of
+    ``gy`` in fp32.  At most 2^24 tokens and outputs; a sum of at most 2^20: ``k`` in the result, the
+    outputs in ``dx``, the tokens in ``dweight`` (in ``dbias`` 2^22).  Each rounding to 8 bits is off by at most half of
     1/127 of its row's (column's) largest value."""
     r = _native.int8_linear(x, weight, bias)
     if r is not None:

@@ -221,3 +221,21 @@ def test_forward_mode_and_tracing_are_refused(path):
             torch.jit.trace(f, (x,), check_trace=False)
         with pytest.raises(RuntimeError, match="trace"):
             make_fx(f)(x)
+
+
+def test_layer_of_more_tokens_than_a_sum_holds(path):
+    # tokens are the sum of the weight's gradient alone: the output, the inputs' gradient and the
+    # bias's take more than 2^20
+    t, m, n, k = torch.bfloat16, (1 << 20) + 77, 8, 16
+    x, w, b, gy = rand((m, k), t, 30).cuda(), rand((n, k), t, 31).cuda(), rand((n,), t, 32).cuda(), rand((m, n), t, 33).cuda()
+    with torch.no_grad():
+        y = prm.int8_linear(x, w, b)
+    assert torch.equal(y[-100:], prm.int8_linear(x[-100:], w, b)) and torch.equal(y[:100], prm.int8_linear(x[:100], w, b))
+    xg, bg, wg = (v.clone().requires_grad_() for v in (x, b, w))
+    gx, gb = torch.autograd.grad(prm.int8_linear(xg, w, bg), (xg, bg), gy)
+    assert torch.equal(gx[-100:], prm.int8_matmul(*prm.quantize_rows(gy[-100:]), *prm.quantize_rows(w, transpose=True), dtype=t))
+    # at most 64 row blocks, rows 8 apart, then the blocks' sums
+    g = gy.double().cpu()
+    check(gb, g.sum(0), (m / 64 / 8 + 8 + 64) * U * g.abs().sum(0) + half(t) * g.sum(0).abs() * (1 + 1e-3) + low(t))
+    with pytest.raises(RuntimeError, match="1048576"):
+        torch.autograd.grad(prm.int8_linear(x, wg), wg, gy)
