@@ -433,7 +433,15 @@ class AuxAdamW:
 def __getattr__(name):
     # the torch.optim adapter and the operators import torch; load them on first use
     if name in ("quantize_rows", "int8_matmul", "int8_linear", "rms_norm"):
-        from . import operators
+        try:
+            from . import operators
+        except (ImportError, PRMError) as e:  # no torch, or no libprm.so: said by the call, so that
+            why = e                           # `import *` still brings what needs neither
+
+            def missing(*args, **kw):
+                raise why
+            missing.__name__ = missing.__qualname__ = name
+            return missing
         fn = globals()[name] = getattr(operators, name)
         return fn
     if name == "PRMOptimizer":

@@ -35,3 +35,22 @@ def test_traces_are_refused(call):
     for mode in ("real", "fake"):
         with pytest.raises(RuntimeError, match="trace"):
             make_fx(f, tracing_mode=mode)(X)
+
+
+@pytest.mark.parametrize("gone", ["torch", "library"])
+def test_import_star_needs_neither_torch_nor_the_library(gone):
+    # the step's names need neither; the operators say what they miss when they are called
+    import subprocess
+    hide = 'sys.modules["torch"] = None' if gone == "torch" else 'import paper_2608_20818_amd as p; p.LIB_PATH = "/nonexistent/libprm.so"'
+    code = f"""import sys
+{hide}
+from paper_2608_20818_amd import *
+assert Config and AdamWConfig and F32 == 0 and rms_norm.__name__ == "rms_norm"
+try:
+    int8_linear(None, None)
+except {"ImportError" if gone == "torch" else "PRMError"} as e:
+    print("said:", e)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and ("torch" if gone == "torch" else "libprm") in r.stdout.split("said:")[1], r.stderr
