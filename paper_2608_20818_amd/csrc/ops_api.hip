@@ -116,30 +116,30 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
   static const char* const call = "prm_quantize_cols";
   TRY(check_type(dtype));
   TRY(check_rows(call, rows, cols, 1, kMaxColRows));
-  if (((cols + 63) / 64) * ((rows + 127) / 128) >= (1ll << 24))  // a grid holds less than 2^32 threads
-    return fail(PRM_EINVAL, "%s: %lld x %lld is too large", call, (long long)rows, (long long)cols);
+  QuantArgs a = {};
+  a.rows = rows;
+  a.cols = cols;
+  QuantJobs jobs = {};
+  jobs.columns[0] = true;
+  jobs.n = 1;
+  jobs.a[0] = a;
+  if (quantize_tiles(jobs) >= kMaxTiles) return fail(PRM_EINVAL, "%s: %lld x %lld is too large", call, (long long)rows, (long long)cols);
   TRY(check_ld(call, "ldx", ldx, cols));
   TRY(check_ld(call, "ldq", ldq, rows));
   TRY(check_workspace(call, workspace, workspace_bytes, prm_quantize_cols_workspace(rows, cols)));
   TRY(check_buffers(call, {{x, "x", size_of(dtype)}, {q, "q", 1}, {scale, "scale", 4}, optional(sum, "sum", size_of(dtype)),
                            {workspace, "workspace", 16}}));
-  QuantArgs a = {};
   a.x = x;
   a.q = q;
   a.scale = scale;
   a.sum = sum;
-  a.rows = rows;
-  a.cols = cols;
   a.ldx = ldx;
   a.ldq = ldq;
   // sums are added in one order, alone or in the layer's gradients
   quantize_cols_blocks(rows, cols, !sum, &a.nrb, &a.rows_per_block);
   a.part_max = (uint32_t*)workspace;
   a.part_sum = (float*)workspace + (int64_t)a.nrb * cols;
-  QuantJobs jobs = {};
   jobs.a[0] = a;
-  jobs.columns[0] = true;
-  jobs.n = 1;
   return launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream));
 }
 
@@ -165,7 +165,9 @@ int prm_internal_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale,
     plan = product_plan(p, true);
     if (!workspace || workspace_bytes < product_workspace(p, plan)) plan = product_plan(p, false);
     if (!product_takes(p, plan))
-      return fail(PRM_EINVAL, "%s: sums over more than %lld need their workspace", call, (long long)kMaxPieceK);
+      return product_takes(p, product_plan(p, true))
+                 ? fail(PRM_EINVAL, "%s: sums over more than %lld need their workspace", call, (long long)kMaxPieceK)
+                 : fail(PRM_EINVAL, "%s: m %lld, n %lld is too large", call, (long long)m, (long long)n);
   } else if (kind < 0 || kind >= PRODUCT_KINDS || !product_takes(p, plan)) {
     return fail(PRM_EINVAL, "%s: kernel %d does not take this product in %d, %d", call, kind, splits, pack);
   }
@@ -187,7 +189,8 @@ uint64_t prm_int8_matmul_workspace(const int8_t* a, int64_t lda, const int8_t* b
   p.m = m;
   p.n = n;
   p.k = k;
-  return product_workspace(p, product_plan(p, true));
+  const ProductPlan plan = product_plan(p, true);
+  return product_takes(p, plan) ? product_workspace(p, plan) : 0;
 }
 
 int prm_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb, const float* b_scale,
@@ -276,6 +279,13 @@ static int check_layer(const char* call, int64_t m, int64_t n, int64_t k) {
   return PRM_OK;
 }
 
+static int too_large(const char* call, int64_t m, int64_t n, int64_t k) {
+  return fail(PRM_EINVAL, "%s: m %lld, n %lld, k %lld is too large", call, (long long)m, (long long)n, (long long)k);
+}
+static int check_plan(const char* call, const ProductArgs& p, const ProductPlan& plan) {
+  return product_takes(p, plan) ? PRM_OK : too_large(call, p.m, p.n, p.k);
+}
+
 uint64_t prm_int8_linear_workspace(int64_t m, int64_t n, int64_t k) {
   return layer_sizes(m, n, k) ? LinearForward(nullptr, nullptr, 0, nullptr, 0, m, n, k).bytes : 0;
 }
@@ -293,14 +303,16 @@ int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
   const LinearForward f((char*)workspace, x, ldx, w, ldw, m, n, k);
   TRY(check_workspace(call, workspace, workspace_bytes, f.bytes));
   const int64_t es = size_of(dtype);
+  const ProductArgs p = product_of(f.x, f.w, m, n, k, bias, y, ldy, f.part);
+  const ProductPlan plan = product_plan(p, true);
+  TRY(check_plan(call, p, plan));
   TRY(check_buffers(call, {{x, "x", es}, {w, "w", es}, optional(bias, "bias", es), {y, "y", es}, {workspace, "workspace", 16}}));
   QuantJobs jobs = {};
   jobs.a[0] = f.x;
   jobs.a[1] = f.w;
   jobs.n = 2;
   TRY(launched(call, launch_quantize((OpType)dtype, jobs, (hipStream_t)hip_stream)));
-  const ProductArgs p = product_of(f.x, f.w, m, n, k, bias, y, ldy, f.part);
-  return launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), (hipStream_t)hip_stream));
+  return launched(call, launch_int8_matmul((OpType)dtype, p, plan, (hipStream_t)hip_stream));
 }
 
 uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
@@ -326,9 +338,6 @@ int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_
   if (!dx && !dw && !db) return PRM_OK;
   const LinearBackward f((char*)workspace, gy, ldgy, x, ldx, w, ldw, m, n, k, db);
   TRY(check_workspace(call, workspace, workspace_bytes, f.bytes));
-  const int64_t es = size_of(dtype);
-  TRY(check_buffers(call, {{gy, "gy", es}, Buf{x, dw ? "x" : nullptr, es}, Buf{w, dx ? "w" : nullptr, es}, optional(dx, "dx", es),
-                           optional(dw, "dw", es), optional(db, "db", es), {workspace, "workspace", 16}}));
   QuantJobs jobs = {};
   const auto add = [&](const QuantArgs& a, bool columns) {
     jobs.columns[jobs.n] = columns;
@@ -340,16 +349,20 @@ int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_
   }
   if (dw || db) add(f.gt, true);
   if (dw) add(f.xt, true);
+  const ProductArgs px = product_of(f.g, f.wt, m, k, n, nullptr, dx, lddx, f.part);
+  const ProductArgs pw = product_of(f.gt, f.xt, n, k, m, nullptr, dw, lddw, f.part);
+  const ProductPlan plan_x = product_plan(px, true), plan_w = product_plan(pw, true);
+  // all that can be refused is, before the first launch
+  if (dx) TRY(check_plan(call, px, plan_x));
+  if (dw) TRY(check_plan(call, pw, plan_w));
+  if (quantize_tiles(jobs) >= kMaxTiles) return too_large(call, m, n, k);
+  const int64_t es = size_of(dtype);
+  TRY(check_buffers(call, {{gy, "gy", es}, Buf{x, dw ? "x" : nullptr, es}, Buf{w, dx ? "w" : nullptr, es}, optional(dx, "dx", es),
+                           optional(dw, "dw", es), optional(db, "db", es), {workspace, "workspace", 16}}));
   hipStream_t s = (hipStream_t)hip_stream;
   TRY(launched(call, launch_quantize((OpType)dtype, jobs, s)));
-  if (dx) {
-    const ProductArgs p = product_of(f.g, f.wt, m, k, n, nullptr, dx, lddx, f.part);
-    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), s)));
-  }
-  if (dw) {
-    const ProductArgs p = product_of(f.gt, f.xt, n, k, m, nullptr, dw, lddw, f.part);
-    TRY(launched(call, launch_int8_matmul((OpType)dtype, p, product_plan(p, true), s)));
-  }
+  if (dx) TRY(launched(call, launch_int8_matmul((OpType)dtype, px, plan_x, s)));
+  if (dw) TRY(launched(call, launch_int8_matmul((OpType)dtype, pw, plan_w, s)));
   return PRM_OK;
 }
 

@@ -50,6 +50,7 @@ struct QuantJobs {
   int32_t n;
 };
 hipError_t launch_quantize(OpType t, const QuantJobs& jobs, hipStream_t s);
+int64_t quantize_tiles(const QuantJobs& jobs);  // of the columns' launch, less than kMaxTiles
 // row blocks of the columns' statistics; alone: of a launch without other quantisers
 void quantize_cols_blocks(int64_t rows, int64_t cols, bool alone, int32_t* nrb, int32_t* rows_per_block);
 

@@ -634,6 +634,8 @@ void launch_piped(const ProductArgs& p, int splits, hipStream_t s) {
   join_kernel<E><<<(unsigned)((p.m * ((p.n + 7) / 8) + 255) / 256), 256, 0, s>>>(p, splits);
 }
 
+int64_t tile_size(ProductKind kind) { return kind == PRODUCT_256 ? 256 : kind == PRODUCT_ANY64 || kind == PRODUCT_64 ? 64 : 128; }
+
 template <class E>
 hipError_t launch(ProductArgs p, const ProductPlan& plan, hipStream_t s) {
   if (plan.pack) {
@@ -653,14 +655,12 @@ hipError_t launch(ProductArgs p, const ProductPlan& plan, hipStream_t s) {
     if (plan.pack & 1) lay(p.a, p.lda, p.m, 0);
     if (plan.pack & 2) lay(p.b, p.ldb, p.n, 1);
     const int64_t pieces = (g.rows[0] + g.rows[1]) * (g.kp / 16);
-    if (pieces >= kMaxTiles * 256) return hipErrorInvalidValue;
     pack_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, s>>>(g);
     if (plan.pack == 3) p.k = g.kp;  // zeros behind both ends: no end within a piece
     p.part = (int32_t*)at;
   }
-  const int64_t b = plan.kind == PRODUCT_256 ? 256 : plan.kind == PRODUCT_ANY64 ? 64 : 128;
+  const int64_t b = tile_size(plan.kind);
   const int64_t tm = (p.m + b - 1) / b, tn = (p.n + b - 1) / b;
-  if (tm * tn >= kMaxTiles) return hipErrorInvalidValue;
   const unsigned tiles = (unsigned)(tm * tn);
   switch (plan.kind) {
     case PRODUCT_FEW: few_kernel<E, 8><<<(unsigned)((p.n + 15) / 16), 512, 0, s>>>(p); break;
@@ -688,6 +688,11 @@ bool product_takes(const ProductArgs& p, const ProductPlan& plan) {
   if (plan.splits != 1 && ((kind != PRODUCT_64 && kind != PRODUCT_128) || plan.splits < 1 || plan.splits > pieces || plan.splits > 64))
     return false;
   if (kind == PRODUCT_FEW) return p.m <= 16;
+  // the launches' grids: tiles, the sums joined and the operands laid out anew
+  const int64_t b = tile_size(kind), packed = (plan.pack & 1 ? p.m : 0) + (plan.pack & 2 ? p.n : 0);
+  if (((p.m + b - 1) / b) * ((p.n + b - 1) / b) >= kMaxTiles) return false;
+  if (plan.splits > 1 && (p.m * ((p.n + 7) / 8) + 255) / 256 >= kMaxTiles) return false;
+  if ((packed * ((p.k + 127) / 128 * 8) + 255) / 256 >= kMaxTiles) return false;
   if (kind == PRODUCT_ANY64 || kind == PRODUCT_ANY128) return true;
   // operands that are laid out anew, or that the direct loads take as they are
   return ((plan.pack & 1) || direct(p.a, p.lda)) && ((plan.pack & 2) || direct(p.b, p.ldb));

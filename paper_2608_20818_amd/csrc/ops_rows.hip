@@ -845,6 +845,8 @@ __global__ __launch_bounds__(256) void quant_columns_kernel(QuantJobs jobs) {
   else col_quant<E, false, OWN>(a, b % gx, b / gx, sh);
 }
 
+int64_t column_tiles(const QuantArgs& a) { return (a.cols + 63) / 64 * ((a.rows + 127) / 128); }
+
 // Blocks that take rows: eight a CU, as many as it holds.
 constexpr int64_t kRowBlocks = 2048;
 
@@ -863,7 +865,7 @@ hipError_t launch_jobs(const QuantJobs& jobs, hipStream_t s) {
       n = (a.cols + 255) / 256 * a.nrb;  // none, where the tiles do it themselves
       const int k = second.n++;
       second.a[k] = a;
-      second.blocks[k] = (int32_t)((a.cols + 63) / 64 * ((a.rows + 127) / 128));
+      second.blocks[k] = (int32_t)column_tiles(a);
     } else {
       n = (groups(a) + per_block - 1) / per_block;
       const int64_t p = (a.cols + 7) / 8, per = a.cols > 512 ? (p + 255) / 256 : 1;
@@ -933,6 +935,13 @@ void quantize_cols_blocks(int64_t rows, int64_t cols, bool alone, int32_t* nrb, 
   per = per < 64 ? 64 : per;
   *rows_per_block = (int32_t)per;
   *nrb = (int32_t)((rows + per - 1) / per);
+}
+
+int64_t quantize_tiles(const QuantJobs& jobs) {
+  int64_t n = 0;
+  for (int j = 0; j < jobs.n; ++j)
+    if (jobs.columns[j]) n += column_tiles(jobs.a[j]);
+  return n;
 }
 
 hipError_t launch_quantize(OpType t, const QuantJobs& jobs, hipStream_t s) {
