@@ -210,9 +210,10 @@ variable_list once(variable_list grads, bool recording) {
   auto refuse = std::make_shared<torch::autograd::DelayedError>("these gradients are not differentiable", (int64_t)grads.size());
   return (*refuse)(std::move(grads));
 }
+// memory that holds the values, in rows (a gradient may be a view that stands for the negative)
 at::Tensor with_rows(const at::Tensor& t, Rows* r) {
-  if (rows_of(t, r)) return t;
-  at::Tensor c = t.contiguous();
+  if (!t.is_neg() && rows_of(t, r)) return t;
+  at::Tensor c = t.resolve_neg().contiguous();
   rows_of(c, r);
   return c;
 }
@@ -318,7 +319,7 @@ struct Norm : torch::autograd::Function<Norm> {
     {
       at::AutoGradMode off(false);
       const variable_list saved = ctx->get_saved_variables();
-      const at::Tensor& w = saved[1];
+      const at::Tensor w = saved[1].defined() ? saved[1].resolve_neg() : saved[1];
       const bool need_dw = w.defined() && ctx->needs_input_grad(1), kept = grads.size() > 1 && grads[1].defined();
       at::Tensor dx;
       if (!grads[0].defined()) {  // only the kept sum has a gradient

@@ -64,7 +64,9 @@ def _same(x, like, shape, what):
 
 def _rows(x):
     """(matrix of the last dimension's rows, its leading dimension): a view where the
-    rows are contiguous and evenly spaced, else a copy."""
+    rows are contiguous and evenly spaced, else a copy.  Its memory holds its values: a view
+    that stands for the negative (conj().imag) is copied."""
+    x = x.resolve_neg()
     c = x.shape[-1]
     if x.dim() != 2:
         x = x.reshape(-1, c) if x.numel() else x.new_empty((x.numel() // max(c, 1), c))
@@ -74,6 +76,7 @@ def _rows(x):
 
 
 def _vector(x):
+    x = x.resolve_neg()
     return x if x.dim() == 1 and (x.stride(0) == 1 or x.shape[0] <= 1) else x.contiguous()
 
 
@@ -193,7 +196,7 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
         out = torch.empty((*a.shape[:-1], n), dtype=dtype, device=a.device)
         m, lda = _rows(a)
         bm, ldb = _rows(b)
-        sa, sb = a_scale.contiguous(), b_scale.contiguous()
+        sa, sb = a_scale.resolve_neg().contiguous(), b_scale.resolve_neg().contiguous()
         bv = None if bias is None else _vector(bias.detach())
         L = load()
         need = L.prm_int8_matmul_workspace(m.data_ptr(), lda, bm.data_ptr(), ldb, rows, n, k)

@@ -239,3 +239,21 @@ def test_layer_of_more_tokens_than_a_sum_holds(path):
     check(gb, g.sum(0), (m / 64 / 8 + 8 + 64) * U * g.abs().sum(0) + half(t) * g.sum(0).abs() * (1 + 1e-3) + low(t))
     with pytest.raises(RuntimeError, match="1048576"):
         torch.autograd.grad(prm.int8_linear(x, wg), wg, gy)
+
+
+@pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
+def test_views_that_stand_for_the_negative(path, t):
+    # contiguous views whose values are the memory's negated (what conj().imag gives of one column)
+    x, r, nw, w, gy = (rand(s, t, 40 + i).cuda() for i, s in enumerate([(6, 24), (6, 24), (24,), (10, 24), (6, 10)]))
+    n = torch._neg_view
+    calls = [(lambda a, b, c: torch.cat(list(prm.rms_norm(a, c, b))), (x, r, nw)),
+             (lambda a, b, c: torch.mul(*[v if v.dim() > 1 else v[:, None] for v in prm.rms_norm(a, c, b, quantize=True)[:2]]), (x, r, nw)),
+             (lambda a: prm.quantize_rows(a)[0], (x,)), (lambda a: prm.quantize_rows(a, transpose=True)[0], (x,)),
+             (lambda a, b, c: prm.int8_linear(a, b, c), (x, w, gy[0])),
+             (lambda a, b, c: prm.int8_matmul(*prm.quantize_rows(x), *prm.quantize_rows(w), bias=c, dtype=t), (x, w, gy[0]))]
+    for f, args in calls:
+        assert torch.equal(f(*[n(a) for a in args]), f(*[-a for a in args]))
+    xg, wg, ng = (v.clone().requires_grad_() for v in (x, w, nw))
+    for f, to, g in ((lambda: prm.int8_linear(xg, wg), (xg, wg), gy), (lambda: prm.rms_norm(xg, ng), (xg, ng), x)):
+        got, want = torch.autograd.grad(f(), to, n(g)), torch.autograd.grad(f(), to, -g)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
