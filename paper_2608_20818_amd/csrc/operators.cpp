@@ -15,6 +15,7 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -117,8 +118,8 @@ PyObject* guarded(F&& f) {
     return f();
   } catch (const Refused& e) {
     return PyLong_FromLong(e.code);
-  } catch (const std::exception& e) {  // out of memory above all
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {  // out of memory above all, or what a hook raised: as torch's own calls raise it
+    torch::translate_exception_to_python(std::current_exception());
     return nullptr;
   }
 }

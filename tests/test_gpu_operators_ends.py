@@ -257,3 +257,22 @@ def test_views_that_stand_for_the_negative(path, t):
     for f, to, g in ((lambda: prm.int8_linear(xg, wg), (xg, wg), gy), (lambda: prm.rms_norm(xg, ng), (xg, ng), x)):
         got, want = torch.autograd.grad(f(), to, n(g)), torch.autograd.grad(f(), to, -g)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_errors_keep_their_type(path):
+    # an allocation that fails, and a hook that raises
+    x, w, nw = (rand(s, torch.float32, 50 + i).cuda().requires_grad_() for i, s in enumerate([(4, 16), (8, 16), (16,)]))
+    q, s = torch.zeros(1 << 20, 16, dtype=torch.int8, device="cuda"), torch.zeros(1 << 20, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):  # 4 TiB of outputs
+        prm.int8_matmul(q, s, q, s, dtype=torch.float32)
+
+    class Told(Exception):
+        pass
+
+    def hook(t):
+        raise Told("no room")
+
+    for f in (lambda: prm.int8_linear(x, w), lambda: prm.rms_norm(x, nw)):
+        with torch.autograd.graph.saved_tensors_hooks(hook, lambda t: t):
+            with pytest.raises(Told, match="no room"):
+                f()
