@@ -387,7 +387,8 @@ int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
  *   dx = Q(gy) Q(w^T)^T   (m x k)      dw = Q(gy^T) Q(x^T)^T   (n x k)
  *   db = the columns' sums of gy       (n values; fp32 in a fixed order)
  * of type dtype; each may be NULL (x is then not read for dw, w not for dx).  m >= 1.
- * `workspace`: prm_int8_linear_backward_workspace(m, n, k) bytes, as above. */
+ * `workspace`: prm_int8_linear_backward_workspace(m, n, k) bytes, as above (of which a call
+ * that asks for some of the gradients uses a part). */
 uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k);
 int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx, const void* w, int64_t ldw,
                              int32_t dtype, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, int64_t m,

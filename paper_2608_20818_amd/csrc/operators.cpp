@@ -25,6 +25,8 @@
 
 #include "../../include/prm.h"
 
+extern "C" uint64_t prm_internal_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k, int32_t dx, int32_t dw, int32_t db);
+
 namespace {
 
 PyObject* g_parameter = nullptr;  // torch.nn.Parameter
@@ -239,7 +241,9 @@ at::Tensor linear(const at::Tensor& x, const at::Tensor& w, const at::Tensor& bi
 
 struct Linear : torch::autograd::Function<Linear> {
   static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, const Maybe& bias) {
-    ctx->save_for_backward({x, w});
+    // each serves the other's gradient alone
+    ctx->save_for_backward({w.requires_grad() ? x : at::Tensor(), x.requires_grad() ? w : at::Tensor()});
+    ctx->saved_data["x"] = x.sizes();
     ctx->saved_data["bias"] = bias.has_value();
     return linear(x, w, or_none(bias));
   }
@@ -249,18 +253,27 @@ struct Linear : torch::autograd::Function<Linear> {
     {
       at::AutoGradMode off(false);
       const variable_list saved = ctx->get_saved_variables();
+      const std::vector<int64_t> sizes = ctx->saved_data["x"].toIntVector();
       Rows rg, rx, rw;
-      const at::Tensor gy = with_rows(grads[0], &rg), x = with_rows(saved[0], &rx), w = with_rows(saved[1], &rw);
-      as_saved(x, gy, rx.rows == rg.rows);
-      as_saved(w, gy, rw.rows == rg.cols && rw.cols == rx.cols);
-      if (ctx->needs_input_grad(0)) out[0] = empty(x.sizes(), x.scalar_type(), x);
-      if (ctx->needs_input_grad(1)) out[1] = empty(w.sizes(), w.scalar_type(), w);
-      if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) out[2] = empty({rw.rows}, w.scalar_type(), w);
-      const uint64_t need = prm_int8_linear_backward_workspace(rx.rows, rw.rows, rx.cols);
-      at::Tensor ws = bytes(need, x);
-      check(prm_int8_linear_backward(gy.const_data_ptr(), rg.ld, x.const_data_ptr(), rx.ld, w.const_data_ptr(), rw.ld,
-                                     code_of(x.scalar_type()), at_of(out[0]), rx.cols, at_of(out[1]), rx.cols, at_of(out[2]), rx.rows,
-                                     rw.rows, rx.cols, at_of(ws), need, stream()));
+      const at::Tensor gy = with_rows(grads[0], &rg);
+      const int64_t m = rg.rows, n = rg.cols, k = sizes.back();
+      at::Tensor x, w;
+      if (ctx->needs_input_grad(0)) {
+        w = with_rows(saved[1], &rw);
+        as_saved(w, gy, rw.rows == n && rw.cols == k);
+        out[0] = empty(sizes, gy.scalar_type(), gy);
+      }
+      if (ctx->needs_input_grad(1)) {
+        x = with_rows(saved[0], &rx);
+        as_saved(x, gy, rx.rows == m && rx.cols == k);
+        out[1] = empty({n, k}, gy.scalar_type(), gy);
+      }
+      if (ctx->saved_data["bias"].toBool() && ctx->needs_input_grad(2)) out[2] = empty({n}, gy.scalar_type(), gy);
+      const uint64_t need = prm_internal_int8_linear_backward_workspace(m, n, k, out[0].defined(), out[1].defined(), out[2].defined());
+      at::Tensor ws = bytes(need, gy);
+      check(prm_int8_linear_backward(gy.const_data_ptr(), rg.ld, x.defined() ? x.const_data_ptr() : nullptr, rx.ld,
+                                     w.defined() ? w.const_data_ptr() : nullptr, rw.ld, code_of(gy.scalar_type()), at_of(out[0]), k,
+                                     at_of(out[1]), k, at_of(out[2]), m, n, k, at_of(ws), need, stream()));
     }
     return once(std::move(out), recording);
   }

@@ -253,18 +253,21 @@ struct LinearForward {
     bytes = l.used;
   }
 };
+// of the gradients asked for
 struct LinearBackward {
-  QuantArgs g, wt, gt, xt;
+  QuantArgs g = {}, wt = {}, gt = {}, xt = {};
   void* part;
   uint64_t bytes;
   LinearBackward(char* base, const void* gp, int64_t ldg, const void* xp, int64_t ldx, const void* wp, int64_t ldw, int64_t m,
-                 int64_t n, int64_t k, void* db) {
+                 int64_t n, int64_t k, bool dx, bool dw, bool with_sum, void* db) {
     Layout l{base};
-    g = quantiser(l, gp, m, n, ldg, false, nullptr);
-    wt = quantiser(l, wp, n, k, ldw, true, nullptr);
-    gt = quantiser(l, gp, m, n, ldg, true, db);
-    xt = quantiser(l, xp, m, k, ldx, true, nullptr);
-    const uint64_t a = part_bytes(m, k, n), b = part_bytes(n, k, m);
+    if (dx) {
+      g = quantiser(l, gp, m, n, ldg, false, nullptr);
+      wt = quantiser(l, wp, n, k, ldw, true, nullptr);
+    }
+    if (dw || with_sum) gt = quantiser(l, gp, m, n, ldg, true, db);
+    if (dw) xt = quantiser(l, xp, m, k, ldx, true, nullptr);
+    const uint64_t a = dx ? part_bytes(m, k, n) : 0, b = dw ? part_bytes(n, k, m) : 0;
     part = l.take(a > b ? a : b);  // the products run one after the other
     bytes = l.used;
   }
@@ -315,8 +318,12 @@ int prm_int8_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
   return launched(call, launch_int8_matmul((OpType)dtype, p, plan, (hipStream_t)hip_stream));
 }
 
+// What the gradients asked for need of prm_int8_linear_backward_workspace.
+uint64_t prm_internal_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k, int32_t dx, int32_t dw, int32_t db) {
+  return layer_sizes(m, n, k) ? LinearBackward(nullptr, nullptr, 0, nullptr, 0, nullptr, 0, m, n, k, dx, dw, db, nullptr).bytes : 0;
+}
 uint64_t prm_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
-  return layer_sizes(m, n, k) ? LinearBackward(nullptr, nullptr, 0, nullptr, 0, nullptr, 0, m, n, k, nullptr).bytes : 0;
+  return prm_internal_int8_linear_backward_workspace(m, n, k, 1, 1, 1);
 }
 
 int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -336,7 +343,7 @@ int prm_int8_linear_backward(const void* gy, int64_t ldgy, const void* x, int64_
     TRY(check_ld(call, "lddx", lddx, k));
   }
   if (!dx && !dw && !db) return PRM_OK;
-  const LinearBackward f((char*)workspace, gy, ldgy, x, ldx, w, ldw, m, n, k, db);
+  const LinearBackward f((char*)workspace, gy, ldgy, x, ldx, w, ldw, m, n, k, dx, dw, db, db);
   TRY(check_workspace(call, workspace, workspace_bytes, f.bytes));
   QuantJobs jobs = {};
   const auto add = [&](const QuantArgs& a, bool columns) {

@@ -334,7 +334,9 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
 class _Int8Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias):
-        ctx.save_for_backward(x, weight)
+        # each serves the other's gradient alone
+        ctx.save_for_backward(x if ctx.needs_input_grad[1] else None, weight if ctx.needs_input_grad[0] else None)
+        ctx.shape = x.shape
         return int8_matmul(*quantize_rows(x), *quantize_rows(weight), bias=bias, dtype=x.dtype)
 
     @staticmethod
@@ -344,16 +346,16 @@ class _Int8Linear(torch.autograd.Function):
         need_x, need_w, need_b = ctx.needs_input_grad
         g = gy.reshape(-1, gy.shape[-1])
         dx = dw = db = None
+        n, k = g.shape[1], ctx.shape[-1]
         if g.shape[0] == 0:
-            return (torch.zeros_like(x) if need_x else None, torch.zeros_like(weight) if need_w else None,
-                    weight.new_zeros(weight.shape[0]) if need_b else None)
+            return (g.new_zeros(ctx.shape) if need_x else None, g.new_zeros(n, k) if need_w else None, g.new_zeros(n) if need_b else None)
         if need_x:
             wq, ws, _ = _quantize_cols(weight, False)
-            dx = int8_matmul(*quantize_rows(g), wq, ws, dtype=x.dtype).reshape(x.shape)
+            dx = int8_matmul(*quantize_rows(g), wq, ws, dtype=g.dtype).reshape(ctx.shape)
         if need_w:
             gq, gs, db = _quantize_cols(g, need_b)
             xq, xs, _ = _quantize_cols(x.reshape(-1, x.shape[-1]), False)
-            dw = int8_matmul(gq, gs, xq, xs, dtype=x.dtype)
+            dw = int8_matmul(gq, gs, xq, xs, dtype=g.dtype)
         elif need_b:
             db = _quantize_cols(g, True)[2]
         return dx, dw, db

@@ -276,3 +276,47 @@ def test_errors_keep_their_type(path):
         with torch.autograd.graph.saved_tensors_hooks(hook, lambda t: t):
             with pytest.raises(Told, match="no room"):
                 f()
+
+
+def test_frozen_parts_of_a_layer_keep_nothing(path):
+    # x serves the weight's gradient alone, the weight the input's: what no gradient needs is not
+    # kept, and may change
+    x, w, b = (rand(s, torch.float32, 60 + i).cuda() for i, s in enumerate([(40, 64), (32, 64), (32,)]))
+    gy = rand((40, 32), torch.float32, 63).cuda()
+    for frozen, leaf in ((w, x), (x, w)):
+        leaf.requires_grad_()
+        want = torch.autograd.grad(prm.int8_linear(x, w, b), leaf, gy)[0]
+        kept = []
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(tuple(t.shape)) or t, lambda t: t):
+            y = prm.int8_linear(x, w, b)
+        assert kept == [tuple(frozen.shape)]
+        with torch.no_grad():
+            leaf.add_(1)
+        assert torch.equal(torch.autograd.grad(y, leaf, gy)[0], want)
+        leaf.requires_grad_(False)
+    b.requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t), lambda t: t):
+        kept.clear()
+        y = prm.int8_linear(x, w, b)
+    assert not kept and torch.equal(torch.autograd.grad(y, b, torch.ones_like(y))[0], torch.full_like(b, 40))
+
+
+def test_gradients_take_the_memory_of_what_is_asked_for():
+    m, n, k, t = 4096, 2048, 1024, torch.bfloat16
+    x, w = rand((m, k), t, 64).cuda(), rand((n, k), t, 65).cuda()
+    gy = rand((m, n), t, 66).cuda()
+
+    def peak(*leaves):
+        for v in (x, w):
+            v.requires_grad_(any(v is u for u in leaves))
+        y = prm.int8_linear(x, w)
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        g = torch.autograd.grad(y, leaves, gy)
+        out = sum(v.numel() * v.element_size() for v in g)
+        return torch.cuda.max_memory_allocated() - before - out
+
+    both, dx, dw = peak(x, w), peak(x), peak(w)
+    # 8-bit operands: gy and w of one, both transposed of the other; a twentieth for scales and statistics
+    assert dx <= 1.05 * (m * n + n * k) + (1 << 20) and dw <= 1.05 * (m * n + m * k) + (3 << 20) and both >= dx
