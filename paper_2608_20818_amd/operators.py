@@ -349,10 +349,12 @@ class _Int8Linear(torch.autograd.Function):
         n, k = g.shape[1], ctx.shape[-1]
         if g.shape[0] == 0:
             return (g.new_zeros(ctx.shape) if need_x else None, g.new_zeros(n, k) if need_w else None, g.new_zeros(n) if need_b else None)
-        if need_x:
+        if need_x:  # hooks may bring back something else
+            _same(weight, g, (n, k), "saved weight")
             wq, ws, _ = _quantize_cols(weight, False)
             dx = int8_matmul(*quantize_rows(g), wq, ws, dtype=g.dtype).reshape(ctx.shape)
         if need_w:
+            _same(x, g, ctx.shape, "saved input")
             gq, gs, db = _quantize_cols(g, need_b)
             xq, xs, _ = _quantize_cols(x.reshape(-1, x.shape[-1]), False)
             dw = int8_matmul(gq, gs, xq, xs, dtype=g.dtype)

@@ -320,3 +320,16 @@ def test_gradients_take_the_memory_of_what_is_asked_for():
     both, dx, dw = peak(x, w), peak(x), peak(w)
     # 8-bit operands: gy and w of one, both transposed of the other; a twentieth for scales and statistics
     assert dx <= 1.05 * (m * n + n * k) + (1 << 20) and dw <= 1.05 * (m * n + m * k) + (3 << 20) and both >= dx
+
+
+def test_saved_tensors_of_a_layer_are_checked(path):
+    # what hooks bring back is what was saved, whichever gradient is asked for
+    x, w = rand((12, 40), torch.float32, 67).cuda(), rand((20, 40), torch.float32, 68).cuda()
+    for wrong in (lambda t: t.half(), lambda t: t.cpu(), lambda t: t[:, :-1], lambda t: t[:-1]):
+        for leaf in (x, w):
+            leaf.requires_grad_()
+            with torch.autograd.graph.saved_tensors_hooks(lambda t: t, wrong):
+                y = prm.int8_linear(x, w)
+            with pytest.raises((RuntimeError, ValueError), match="saved "):
+                torch.autograd.grad(y.sum(), leaf)
+            leaf.requires_grad_(False)
