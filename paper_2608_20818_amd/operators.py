@@ -273,9 +273,8 @@ class _RmsNorm(torch.autograd.Function):
     def backward(ctx, gy, gh=None):
         h, weight = ctx.saved_tensors
         need_dw = weight is not None and ctx.needs_input_grad[1]
-        if gy is None:  # only the kept sum has a gradient
-            dw = torch.zeros_like(weight) if need_dw else None
-            return (gh if ctx.needs_input_grad[0] else None), dw, (gh if ctx.needs_input_grad[2] else None), None
+        if gy is None:  # only the kept sum has a gradient, in which the weight takes no part
+            return (gh if ctx.needs_input_grad[0] else None), None, (gh if ctx.needs_input_grad[2] else None), None
         _same(h, gy, gy.shape, "saved input")  # hooks may bring back something else
         if weight is not None:
             _same(weight, gy, gy.shape[-1:], "saved weight")

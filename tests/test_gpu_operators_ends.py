@@ -333,3 +333,11 @@ def test_saved_tensors_of_a_layer_are_checked(path):
             with pytest.raises((RuntimeError, ValueError), match="saved "):
                 torch.autograd.grad(y.sum(), leaf)
             leaf.requires_grad_(False)
+
+
+def test_gradient_of_the_kept_sum_alone(path):
+    # the weight takes no part in the kept sum, so it has no gradient, not one of zeros that a step
+    # with weight decay would take
+    x, w, r = (rand(s, torch.float32, 70 + i).cuda().requires_grad_() for i, s in enumerate([(7, 33), (33,), (7, 33)]))
+    prm.rms_norm(x, w, r)[1].sum().backward()
+    assert w.grad is None and (x.grad == 1).all() and (r.grad == 1).all()
