@@ -341,3 +341,68 @@ def test_gradient_of_the_kept_sum_alone(path):
     x, w, r = (rand(s, torch.float32, 70 + i).cuda().requires_grad_() for i, s in enumerate([(7, 33), (33,), (7, 33)]))
     prm.rms_norm(x, w, r)[1].sum().backward()
     assert w.grad is None and (x.grad == 1).all() and (r.grad == 1).all()
+
+
+# ---------------------------------------------------------------- many rows
+@pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("shape", [(9000, 64), (2100, 600), (1100, 2056), (2300, 4090), (700, 4104), (600, 9000), (600, 17000), (600, 33000)], ids=str)
+def test_norm_gradients_of_several_rows_a_block(shape, t):
+    # on the GPU in 64 bits, as these are too many for the host
+    x, w, gy, gh = (rand(s, t, 80 + i).cuda() for i, s in enumerate([shape, shape[1:], shape, shape]))
+    for kept, need_w in ((True, True), (False, True), (True, False)):
+        xg, wg = x.clone().requires_grad_(), w.clone().requires_grad_(need_w)
+        to = (xg, wg) if need_w else (xg,)
+        if kept:
+            got = torch.autograd.grad(prm.rms_norm(xg, wg, torch.zeros_like(x)), to, (gy, gh))
+        else:
+            got = torch.autograd.grad(prm.rms_norm(xg, wg), to, gy)
+        h = x.double()
+        r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6)
+        g, n = gy.double() * w.double(), h * r
+        dx = r * (g - n * (g * n).mean(1, keepdim=True))
+        size = r * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True))
+        if kept:
+            dx, size = dx + gh.double(), size + gh.double().abs()
+        s = sums(shape[1])
+        check(got[0], dx.cpu(), ((2.5 * s + 20) * U * size + half(t) * dx.abs() * (1 + 1e-3) + low(t)).cpu())
+        if need_w:
+            dw, size = (gy.double() * n).sum(0), (gy.double() * n).abs().sum(0)
+            check(got[1], dw.cpu(), ((s / 2 + 6 + additions(*shape, t)) * U * size + half(t) * dw.abs() * (1 + 1e-3) + low(t)).cpu())
+
+
+@pytest.mark.parametrize("t", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("mnk", [(2500, 600, 1000), (2100, 40, 5000), (3001, 2100, 520), (2300, 24, 17000), (9001, 513, 48)], ids=str)
+def test_linear_of_several_rows_a_block(mnk, t):
+    # one call of the layer takes rows in turn where they are many: the bits of its parts, and the
+    # parts those of the definition
+    m, n, k = mnk
+    x, w, gy = rand((m, k), t, 90).cuda(), rand((n, k), t, 91, 0.02).cuda(), rand((m, n), t, 92, 1e-2).cuda()
+    xg, wg = x.clone().requires_grad_(), w.clone().requires_grad_()
+    y = prm.int8_linear(xg, wg)
+    gx, gw = torch.autograd.grad(y, (xg, wg), gy)
+    assert torch.equal(y, prm.int8_matmul(*prm.quantize_rows(x), *prm.quantize_rows(w), dtype=t))
+    assert torch.equal(gx, prm.int8_matmul(*prm.quantize_rows(gy), *prm.quantize_rows(w, transpose=True), dtype=t))
+    assert torch.equal(gw, prm.int8_matmul(*prm.quantize_rows(gy, transpose=True), *prm.quantize_rows(x, transpose=True), dtype=t))
+    for v in (x, gy):
+        for a, b in ((prm.quantize_rows(v), eight(v.double().cpu())), (prm.quantize_rows(v, transpose=True), eight(v.double().cpu().t()))):
+            assert torch.equal(a[0].cpu().double(), b[0])
+            check_scale(a[1], b[1])
+
+
+def test_rows_of_more_than_one_launch():
+    # over 2^21 rows a kernel runs in slices
+    t, rows, cols = torch.bfloat16, (1 << 21) + 4099, 24
+    x, r, w = rand((rows, cols), t, 100).cuda(), rand((rows, cols), t, 101).cuda(), rand((cols,), t, 102).cuda()
+    q, s = prm.quantize_rows(x)
+    y, h = prm.rms_norm(x, w, r)
+    q8, s8, h8 = prm.rms_norm(x, w, r, quantize=True)
+    assert torch.equal(h, h8) and torch.equal(h, (x.float() + r.float()).to(t))
+    for at in (slice(0, 300), slice((1 << 21) - 300, (1 << 21) + 300), slice(rows - 300, rows)):
+        for a, b in ((q, s), (q8, s8)):
+            assert a.shape == (rows, cols) and b.shape == (rows,)
+        assert all(torch.equal(a, b) for a, b in zip((q[at], s[at]), prm.quantize_rows(x[at])))
+        assert all(torch.equal(a, b) for a, b in zip((y[at], h[at]), prm.rms_norm(x[at], w, r[at])))
+        assert all(torch.equal(a, b) for a, b in zip((q8[at], s8[at], h8[at]), prm.rms_norm(x[at], w, r[at], quantize=True)))
+    qe, se = eight(x.double().cpu())
+    assert torch.equal(q.cpu().double(), qe)
+    check_scale(s, se)
