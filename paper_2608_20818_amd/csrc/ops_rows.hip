@@ -405,7 +405,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
     for (int k = 0; k < 8; ++k) {
       v[k] *= down;
       d[k] = with_dw ? d[k] + g[k] * (v[k] * r) : d[k];
-      o[k] = r * down * (g[k] * f[k] - v[k] * coef);
+      o[k] = r * (g[k] * f[k] - v[k] * coef) * down;
     }
     if (a.gh) {
       E::expand(xs, v);
@@ -483,7 +483,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_grad_kernel(NormGr
       joined(ss, sg);
       if (ss < inf && fabsf(sg) < inf) continue;
       const bool with_dw = !(ss < inf);
-      constexpr float down = 0x1p-64f;
+      constexpr float down = 0x1p-80f;  // 2^24 squares of 2^128 come to 2^120
       swept(row, down, ss, sg);
       joined(ss, sg);
       const float r = 1.f / sqrtf(ss / (float)cols + a.eps * down * down);

@@ -76,8 +76,8 @@ def test_norm_past_the_range_of_squares(shape, t):
     # rows whose squares leave fp32's range beside ordinary ones, plain and in 8 bits, with products
     # h w that leave it at either end too
     x, res = rand(shape, t, 1), rand(shape, t, 2)
-    up = torch.tensor([2.0 ** e for e in (70, 0, 100, 120, 63)], dtype=torch.float64)
-    by = up[torch.arange(shape[0]) % 5][:, None]
+    up = torch.tensor([2.0 ** e for e in (125, 0, 70, 100, 120, 63)], dtype=torch.float64)
+    by = up[torch.arange(shape[0]) % 6][:, None]
     x, res = (x.double() * by).to(t), (res.double() * by).to(t)
     for scale in (1.0, 2.0 ** 60, 2.0 ** -120):
         w = rand(shape[1:], t, 3, scale)
@@ -141,11 +141,11 @@ def additions(rows, cols, t):
 @pytest.mark.parametrize("shape", WIDE, ids=str)
 def test_norm_gradients_past_the_range_of_squares(shape, t):
     # the rows as above; gradients of about the norm's own size, so that r g stays a normal number.
-    # A value below 2^-62 of a row scaled by 2^-64 may round in fp32's lowest range: 2^-150 of it,
-    # times r 2^64 <= 2^12: below 2^-138 |gy| in n
+    # A value below 2^-46 of a row scaled by 2^-80 may round in fp32's lowest range, by 2^-150, in n
+    # times r 2^80, where r is at most 2^-52 (2^24 squares past 2^128): below 2^-122
     x = rand(shape, t, 8)
-    up = torch.tensor([2.0 ** e for e in (70, 0, 100, 120, 63)], dtype=torch.float64)
-    by = up[torch.arange(shape[0]) % 5][:, None]
+    up = torch.tensor([2.0 ** e for e in (125, 0, 70, 100, 120, 63)], dtype=torch.float64)
+    by = up[torch.arange(shape[0]) % 6][:, None]
     x, w, gy, gh = (x.double() * by).to(t), rand(shape[1:], t, 9), rand(shape, t, 10), rand(shape, t, 11)
     for kept in (False, True):
         xg, wg, rg = x.cuda().requires_grad_(), w.cuda().requires_grad_(), torch.zeros_like(x).cuda()
@@ -164,7 +164,7 @@ def test_norm_gradients_past_the_range_of_squares(shape, t):
         check(got[0], dx, (2.5 * s + 20) * U * size + half(t) * dx.abs() * (1 + 1e-3) + low(t))
         dw, size = (gy.double() * n).sum(0), (gy.double() * n).abs().sum(0)
         check(got[1], dw, (s / 2 + 6 + additions(*shape, t)) * U * size + half(t) * dw.abs() * (1 + 1e-3) + low(t)
-              + 2.0 ** -138 * gy.double().abs().sum(0))
+              + 2.0 ** -122 * gy.double().abs().sum(0))
 
 
 @pytest.mark.parametrize("shape", [(7, 40), (1030, 2050), (300, 4100), (5, 33000)], ids=str)
