@@ -357,8 +357,8 @@ int prm_quantize_cols(const void* x, int32_t dtype, int64_t rows, int64_t cols, 
 
 /* out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] b[j][k] + bias[j], for a
  * (m x k: tokens), b (n x k: output channels, as a linear layer's weight is kept)
- * and out (m x n, type dtype).  The sum is exact (whole numbers), the rest fp32, rounded
- * once.  1 <= k <= 2^20, 0 <= m, n <= 2^24.  bias: n values of type dtype, or NULL.
+ * and out (m x n, type dtype).  The sum is exact (whole numbers), a_scale, b_scale and bias
+ * are applied in this order in fp32, the result is rounded once.  1 <= k <= 2^20, 0 <= m, n <= 2^24.  bias: n values of type dtype, or NULL.
  * `workspace`: prm_int8_matmul_workspace(the same operands and sizes) bytes, 16-byte
  * aligned, used by this call only: a product with few outputs and a long sum is split
  * there, and operands whose rows do not start on 16-byte boundaries may be laid out

@@ -528,9 +528,9 @@ __global__ __launch_bounds__(256) void piped_kernel(ProductArgs p, int tiles_m, 
 // ---------------------------------------------------------------------------
 // few tokens (at most 16): 16 channels a block, read once and straight into registers;
 // the block's waves split k and join their sums in shared memory.  One token through 20480
-// x 5120: 22 us (4.8 TB/s; bound by reading the weight).  Every block reads the tokens
-// from its L2, which 16 of them feel (33 us); two or four times the channels a block were
-// no faster (32, 33 us).
+// x 5120: 20 us (5.2 TB/s; bound by reading the weight), 8 tokens 26.  Every block reads the tokens
+// from its L2, which 16 of them feel (31 us; two or four times the channels a block were
+// no faster).
 // ---------------------------------------------------------------------------
 template <class E, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(ProductArgs p) {

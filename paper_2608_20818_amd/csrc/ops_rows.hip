@@ -7,13 +7,15 @@
 //               from q = rn(127 h w / max |h w|) and stays in the scale r max |h w| / 127
 //   gradient    n = h r, g = gy w:  dx = r (g - n mean(g n)) + gh,  dw = sum over rows of gy n
 //
-// All are bound by HBM: each element is read once and held in registers as stored
-// until the row's statistics are there (rows of at most 32768 elements; longer ones
-// are swept again).  A thread holds pieces of 8 elements, so that an access of 16-bit
-// values is 16 bytes a lane and one contiguous span a wave, at any alignment.
-// bf16, bytes moved: norm with the residual 8192 x 5120 62 us (5.4 TB/s), its gradient
-// 8192 x 4096 54 us (5.0 TB/s), rows in 8 bits 10240 x 2560 15 us (5.4 TB/s), columns
-// 4096 x 5120 25 us in two sweeps; a copy reaches 4.96 TB/s.
+// All are bound by HBM.  The norm, its gradient and the quantiser of rows read each element once
+// and hold it in registers as stored until the row's statistics are there (rows of at most
+// 32768 elements, in the layer's launch of several quantisers 16384; longer ones are swept again);
+// the quantiser of columns reads a matrix twice.  A thread holds pieces of 8 elements, so that an
+// access of 16-bit values is 16 bytes a lane and one contiguous span a wave, at any alignment.
+// bf16, bytes moved: norm with the residual 8192 x 5120 61 us (5.5 TB/s), with 8-bit output 58 us
+// (5.0 TB/s; fp16 56, fp32 106 us), its gradient 8192 x 4096 54 us (5.0 TB/s), rows in 8 bits
+// 10240 x 2560 15 us (5.4 TB/s), columns 4096 x 5120 25 us; a copy of 4 GiB reaches 6.5 TB/s, three
+// streams in and two out 5.65.
 #include <type_traits>
 
 #include "ops_device.h"

@@ -168,9 +168,10 @@ def int8_matmul(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16):
     """``a_scale a (b_scale b)^T + bias``: the product of 8-bit operands, ``a``
     ``[..., k]`` with a scale for each row (token) and ``b`` ``[n, k]`` with one for each
     row (output channel, as a linear layer's weight is kept; rows on 16-byte boundaries, as
-    ``quantize_rows`` gives them, are the fast ones); ``bias`` ``[n]`` and the result ``[..., n]`` are of type ``dtype``.  The sum over k (at most 2^20) is exact;
-    scales and bias are applied in fp32 and the result rounded once.  Not
-    differentiable (``int8_linear`` is)."""
+    ``quantize_rows`` gives them, are the fast ones); ``bias`` ``[n]`` and the result ``[..., n]`` are
+    of type ``dtype``.  The sum over k (at most 2^20) is exact; ``a_scale``, ``b_scale`` and
+    bias are applied in this order in fp32 and the result rounded once.  Not differentiable
+    (``int8_linear`` is)."""
     r = _native.int8_matmul(a, a_scale, b, b_scale, bias, _CODE.get(dtype, -1))
     if r is not None:
         return _check(r) if type(r) is int else r
@@ -303,7 +304,8 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = 
     Returns ``y``, or ``(y, h)`` with a residual; with ``quantize`` the norm in 8 bits,
     ``(q, scale)`` or ``(q, scale, h)``, for ``int8_matmul``.  ``weight`` ``[cols]`` and
     ``residual`` (shaped as x) have x's type.  The plain outputs are differentiable in
-    x, weight and residual; the 8-bit ones are not."""
+    x, weight and residual; the 8-bit ones are not.  Sums over a row are taken in fp32, where
+    they leave its range in fp64 or scaled."""
     eps = float(eps)
     r = _native.rms_norm(x, weight, residual, eps, quantize)
     if r is not None:
@@ -368,9 +370,9 @@ def int8_linear(x, weight, bias=None):
     result ``[..., n]`` has.  Its gradients are those of the unquantised layer, their
     products in 8 bits too, each operand quantised along the sum it enters:
     ``dx = Q(gy) Q(weight^T)^T``, ``dweight = Q(gy^T) Q(x^T)^T``, ``dbias`` the sum of
-    ``gy`` in fp32.  At most 2^24 tokens and outputs; a sum of at most 2^20: ``k`` in the result, the
-    outputs in ``dx``, the tokens in ``dweight`` (in ``dbias`` 2^22).  Each rounding to 8 bits is off by at most half of
-    1/127 of its row's (column's) largest value."""
+    ``gy`` in fp32.  At most 2^24 tokens and outputs; a sum of at most 2^20: ``k`` in the
+    result, the outputs in ``dx``, the tokens in ``dweight`` (in ``dbias`` 2^22).  Each rounding
+    to 8 bits is off by at most half of 1/127 of its row's (column's) largest value."""
     r = _native.int8_linear(x, weight, bias)
     if r is not None:
         return _check(r) if type(r) is int else r
